@@ -38,9 +38,30 @@
  *  Token t of request b lives in page block_table[b][t / 16], slot t % 16.
  *  Element types: bf16, or OCP fp8 e4m3fn with one fp32 dequantisation
  *  scale per (request, KV head) for K and one for V (real value =
- *  e4m3fn(code) * scale).  Supported: head_dim D in {64, 128}; H_q a
- *  multiple of H_kv with G = H_q / H_kv <= 16; query head h reads KV head
- *  h / G.
+ *  e4m3fn(code) * scale), or 4 bits (below).  Supported: head_dim D in {64,
+ *  128}; H_q a multiple of H_kv with G = H_q / H_kv <= 16; query head h reads
+ *  KV head h / G.
+ *
+ * 4-bit pools: K and V [NP, H_kv, 17, D/2] bytes, dtype BELLMAN_FP4_E2M1 (two
+ *  codes a byte; shapes and strides count bytes).  A tile (page, head) is 8 D
+ *  bytes of e2m1 codes and D/2 scale bytes: every 32 consecutive dims of a
+ *  token share an E8M0 scale, value = e2m1(code) * 2^(scale - 127), scale 255 =
+ *  NaN.  In a tile, slot s and dim d lie at byte
+ *    K code   (d / 32) 256 + 16 s + (d % 32) / 2, low nibble for even d
+ *    K scale  8 D + 16 (d / 32) + s
+ *    V code   (16 (s / 4) + d % 16) D/8 + 2 (d / 16) + (s % 4) / 2, low nibble
+ *             for even s
+ *    V scale  8 D + (s / 4) D/8 + 4 (d / 32) + s % 4
+ *  (integer divisions): K as the matrix cores take it, V by the four slots and
+ *  sixteen dims that a lane of the decode kernel holds.  1.0625 D bytes a
+ *  token of one head, K and V together.
+ *  Quantisation, wherever bf16 rows enter these pools: a block whose largest
+ *  magnitude is m 2^e, 1 <= m < 2, takes the scale 2^(e - 2), or 2^(e - 1)
+ *  where m > 1.75 (so that no value is off by more than half the widest step),
+ *  kept within 2^-127 .. 2^125; each value over the scale is rounded to the
+ *  nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even code, 6 at most,
+ *  its sign kept.  A block with an infinity or a NaN gets scale 255 and codes
+ *  0: it reads as NaN.
  */
 #ifndef BELLMAN_H
 #define BELLMAN_H
@@ -63,7 +84,8 @@ typedef enum bellman_dtype {
     BELLMAN_BF16 = 1,
     BELLMAN_FP8_E4M3FN = 2,
     BELLMAN_INT32 = 3,
-    BELLMAN_FP32 = 4
+    BELLMAN_FP32 = 4,
+    BELLMAN_FP4_E2M1 = 5           /* 4-bit pools: bytes of two codes, and scale bytes */
 } bellman_dtype_t;
 
 #define BELLMAN_MAX_DIMS 5
@@ -90,8 +112,10 @@ typedef struct bellman_tensor {
  *                 dequant_scale (K's for k_new, V's for v_new), the quotient
  *                 one correctly rounded binary32 division, rounded to
  *                 nearest with ties to the even mantissa, saturating at
- *                 +-448, NaN kept.
- *   k_pages       [NP, H_kv, D/x, 16, x] contiguous (written).
+ *                 +-448, NaN kept.  4-bit pools take bf16 rows and quantise
+ *                 them as stated above.
+ *   k_pages       [NP, H_kv, D/x, 16, x] contiguous (written); 4-bit pools
+ *                 [NP, H_kv, 17, D/2], here and in every call below.
  *   v_pages       [NP, H_kv, D, 16] contiguous (written).
  *   block_table   int32 [B, maxP], innermost contiguous; the page that will
  *                 receive the token must already be assigned.
@@ -103,7 +127,8 @@ typedef struct bellman_tensor {
  * changes nothing else: the bytes around the new slot that share a 32-byte
  * sector with it (the neighbouring slot's K chunk, the rest of each V dim
  * row) are read and written back unchanged, so that every sector is written
- * whole.  Hence no two requests of one call may append into the same page.
+ * whole (4-bit pools: the nibbles of V that share the new ones' 16-byte words).
+ * Hence no two requests of one call may append into the same page.
  * A request whose slot lies outside the block table or the pool is skipped
  * (no byte written, length unchanged) and flagged in the device error word.
  */
@@ -118,13 +143,17 @@ int bellman_kv_append(const bellman_tensor_t *k_new, const bellman_tensor_t *v_n
  * over the request's KV pages (query head h uses KV head h / G).
  *   q            bf16 [B, H_q, D], innermost contiguous.
  *   k_pages      [NP, H_kv, D/x, 16, x] contiguous, bf16 or fp8 (with
- *                dequant_scale set).
+ *                dequant_scale set), or 4-bit (no dequant_scale).
  *   v_pages      [NP, H_kv, D, 16] contiguous, same element type.
  *   block_table  int32 [B, maxP], innermost contiguous.
  *   seq_lens     int32 [B]: attention lengths (after this step's append).
  *   scale        finite fp32 softmax scale (usually 1/sqrt(D)).
  *   out          bf16 [B, H_q, D], innermost contiguous (written; rounded to
  *                nearest even).  A request of length 0 gets zeros.
+ * Over 4-bit pools the keys enter the matrix cores as they lie; the values'
+ * scales go into the weights, held as the sum of two bf16 (2^-14 relative),
+ * whose scaled magnitudes below 2^-126 count as 0.  A NaN key block makes its
+ * (request, head)'s rows NaN, a NaN value block its 32 dims of them.
  * The work of the batch, as (request, KV head, step of consecutive pages)
  * units, is dealt to the GPU's resident wavefronts in equal contiguous
  * shares; a request cut by a share boundary has its partial softmax
@@ -168,15 +197,15 @@ typedef struct bellman_attn_opts {
                              1..255 = weights 256 + k : 256 - k.  Results agree
                              within rounding. */
     int32_t pages_per_step; /* 16-token pages per softmax update: 1 or 2 (bf16),
-                               1, 2 or 4 (fp8); 0 = the library's choice
-                               (4 for fp8 pools; for bf16 pools 1 when
+                               1, 2 or 4 (fp8), 4 (4-bit); 0 = the library's choice
+                               (4 for fp8 and 4-bit pools; for bf16 pools 1 when
                                B * H_kv * maxP is below 512 pages per wave,
                                else 2; at head_dim 64 also 2 below 64 pages
                                where pipeline_depth is 0 too) */
     int32_t pipeline_depth; /* steps of pages in flight per wavefront while it
                                computes one: 1 (up to two wavefronts per SIMD) or 2
                                (one per SIMD); 0 = the library's choice (1 for
-                               fp8 pools; for bf16 pools 2, or 1 where
+                               fp8 and 4-bit pools; for bf16 pools 2, or 1 where
                                pages_per_step is 0 too and B * H_kv * maxP is
                                below 512 pages per wave, 64 at head_dim 64) */
     void *event_begin;    /* optional hipEvent_t recorded on the stream right before
@@ -256,7 +285,9 @@ int bellman_decode_attention_noalloc(const bellman_tensor_t *q, const bellman_te
  * default steps only (opts pages_per_step 0, 1 or 2 and pipeline_depth 0 or
  * 2 over bf16 pools; pages_per_step 0 or 4 and pipeline_depth 0 or 1 over
  * fp8 pools) and without wave_times; other options return
- * BELLMAN_ERR_UNSUPPORTED before anything is written.  Same workspace and
+ * BELLMAN_ERR_UNSUPPORTED before anything is written.  Over 4-bit pools the
+ * call makes the two calls' launches: their results in every case, nothing
+ * enqueued where either would be refused.  Same workspace and
  * graph-capture properties as bellman_decode_attention_opts. */
 int bellman_decode_step(const bellman_tensor_t *k_new, const bellman_tensor_t *v_new,
                         const bellman_tensor_t *q, bellman_tensor_t *k_pages,
@@ -278,12 +309,13 @@ int bellman_decode_step(const bellman_tensor_t *k_new, const bellman_tensor_t *v
 /* Write n_b new tokens per request at positions seq_lens[b] .. seq_lens[b] +
  * n_b - 1 (page block_table[b][pos / 16], slot pos % 16), then set
  * seq_lens[b] += n_b.
- *   k_new, v_new  [T, H_kv, D] in the pools' element type, innermost
+ *   k_new, v_new  [T, H_kv, D] in the pools' element type (bf16 for 4-bit
+ *                 pools, quantised as stated above), innermost
  *                 contiguous, rows 16-byte aligned; T = q_start[B].
  *   k_pages, v_pages, block_table: as for bellman_kv_append; the pages of
  *                 every new position must already be assigned.
  *   seq_lens      int32 [B] contiguous (read, then advanced).
- * Byte-exact copies; nothing else is written.  A token outside its
+ * Byte-exact copies (or that quantisation); no other slot changes.  A token outside its
  * request's table or the pool is skipped and flagged (flag 1), and that
  * request's length is left unchanged when its last position does not fit.
  * Once the workspace has grown to the call's size, the call enqueues only
@@ -292,6 +324,61 @@ int bellman_kv_write(const bellman_tensor_t *k_new, const bellman_tensor_t *v_ne
                      bellman_tensor_t *k_pages, bellman_tensor_t *v_pages,
                      const bellman_tensor_t *block_table, bellman_tensor_t *seq_lens,
                      const bellman_tensor_t *q_start, void *stream);
+
+/* The rows that the cache holds: request b's last n_b = q_start[b+1] -
+ * q_start[b] of its L_b = seq_lens[b] cached tokens (a write's new rows when it
+ * follows the write; whole requests when n_b = L_b), for sharing, moving or
+ * checking cached requests.
+ *   k_out, v_out  bf16 [T, H_kv, D] (written), innermost contiguous, rows
+ *                 16-byte aligned; row q_start[b] + i is token L_b - n_b + i.
+ * bf16 pools: copies.  fp8 pools (dequant_scale required): code * scale in
+ * binary32, rounded to nearest even.  4-bit pools: the exact values (all bf16
+ * numbers; beyond bf16's range infinite).  A token whose page lies outside the
+ * pool reads as NaN (flag 4); rows of a malformed request (n_b < 0, n_b > L_b,
+ * rows past T, L_b past the table) are not written (flag 2), and a q_start
+ * that decreases, starts below 0 or ends past T reads no row at all.  Workspace
+ * and graph capture as for bellman_kv_write. */
+int bellman_kv_read(const bellman_tensor_t *k_pages, const bellman_tensor_t *v_pages,
+                    const bellman_tensor_t *block_table, const bellman_tensor_t *seq_lens,
+                    const bellman_tensor_t *q_start, bellman_tensor_t *k_out,
+                    bellman_tensor_t *v_out, void *stream);
+
+/* Norm and rotation of queries and keys, the step between their projections
+ * and the cache:
+ *   y = x / sqrt(mean_d(x_d^2) + eps) * (w + weight_offset)   (where w is given)
+ *   (y_i, y_j) -> (y_i cos a - y_j sin a, y_j cos a + y_i sin a),
+ *                 a = position * inv_freq[f],  f < F
+ * for every token and head, with R = 2 F <= D rotated dims: pairs
+ * (i, j) = (f, f + F), or (2 f, 2 f + 1) with opts->interleaved; dims R .. D-1
+ * are not turned.
+ *   q, k          bf16 [T, H_q, D], [T, H_kv, D], innermost contiguous, rows
+ *                 16-byte aligned (views of a joint projection's rows do); D in
+ *                 {64, 128}.
+ *   q_weight, k_weight  [D] bf16 or fp32, contiguous, or NULL: that tensor is
+ *                 rotated without a norm.
+ *   positions     int32 [T], or [axes, T] with the tokens contiguous: any
+ *                 value.  With several axes (time, height, width of images and
+ *                 video) axis 0 turns the first sections[0] frequencies, axis
+ *                 1 the next sections[1], and so on; they sum to F.
+ *   inv_freq      fp32 [F], contiguous, F a multiple of 8.
+ *   q_out, k_out  bf16, shaped as q and k (written, rounded to nearest even):
+ *                 q and k themselves, or memory that overlaps no input.
+ * Angles are formed in binary64, everything else in binary32.  Enqueues one
+ * kernel, needs no workspace (graph-capturable).  opts NULL: eps 1e-6, no
+ * offset, one axis, pairs (f, f + F). */
+typedef struct bellman_rope_opts {
+    float eps;                /* >= 0, used as given */
+    float weight_offset;      /* added to the weights (1 for weights stored less one) */
+    int32_t interleaved;      /* 0 or 1 */
+    int32_t axes;             /* 1 to 4 (0 = 1) */
+    int32_t sections[4];      /* frequencies of each axis, where axes > 1 */
+} bellman_rope_opts_t;
+
+int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
+                         const bellman_tensor_t *q_weight, const bellman_tensor_t *k_weight,
+                         const bellman_tensor_t *positions, const bellman_tensor_t *inv_freq,
+                         bellman_tensor_t *q_out, bellman_tensor_t *k_out,
+                         const bellman_rope_opts_t *opts, void *stream);
 
 /* Causal prompt attention over the paged cache: request b's query rows are
  * its last n_b of L_b = seq_lens[b] cached tokens, and the row of token
@@ -324,10 +411,14 @@ int bellman_kv_write(const bellman_tensor_t *k_new, const bellman_tensor_t *v_ne
  * (values more than 2^63 below the largest of a key range lose bits).  Over fp8 pools the
  * codes are staged in LDS as bytes and widened exactly at the operand load
  * (K to bf16, V to fp16); the K scale folds into the softmax scale and the
- * V scale into the final normalisation.  Scratch in the per-device
+ * V scale into the final normalisation.  Over 4-bit pools the keys the call
+ * reads are copied too, widened exactly to bf16, and the values to fp16 as over
+ * bf16 pools; a page outside the pool makes the rows that see it NaN.  Scratch
+ * in the per-device
  * workspace: 3 KiB + 4 (B + 1) bytes; over bf16 pools, for the value copy
  * and its bookkeeping, B ceil(maxP / 4) (4 + 4 H_kv + 128 D H_kv) +
- * 4 (B + 1) bytes more (maxP = the block table's width); and where keys are
+ * 4 (B + 1) bytes more (maxP = the block table's width), over 4-bit pools
+ * B ceil(maxP / 4) 128 D H_kv more than that; and where keys are
  * shared out 128 (4 D + 8) bytes a share, at most four shares a CU (a capture
  * with no room for those, or a call whose device has no memory for them, runs
  * uncut; results agree within rounding).  Like

@@ -16,6 +16,7 @@ from ._binding import (  # noqa: F401
     decode_step,
     device_errors,
     kv_append,
+    kv_read,
     kv_write,
     last_error,
     length_cap,
@@ -23,6 +24,7 @@ from ._binding import (  # noqa: F401
     library_path,
     prefill_attention,
     probe_gather,
+    qk_norm_rope,
     reserve_workspace,
     shutdown,
     version,

@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # _marshal.so beside it
 _LIB_PATH = os.environ.get("BELLMAN_LIBRARY") or os.path.join(_HERE, "libbellman.so")
 
-BF16, FP8_E4M3FN, INT32, FP32 = 1, 2, 3, 4
+BF16, FP8_E4M3FN, INT32, FP32, FP4_E2M1 = 1, 2, 3, 4, 5
 MAX_DIMS = 5
 FIXED_SCRATCH_BYTES = 32 << 20     # BELLMAN_FIXED_SCRATCH_BYTES
 
@@ -51,6 +51,11 @@ class AttnOpts(ctypes.Structure):
 
 class PrefillOpts(ctypes.Structure):
     _fields_ = [("event_begin", ctypes.c_void_p), ("event_end", ctypes.c_void_p)]
+
+
+class RopeOpts(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("interleaved", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4)]
 
 
 CTL_LINEAR, CTL_MPC, CTL_BBR, CTL_PCC = 1, 2, 3, 4
@@ -95,7 +100,7 @@ _warned = False         # that it is None
 _addr = {}              # entry point -> its address, for _marshal.call
 
 # the forms of call (marshal.cpp)
-_APPEND, _DECODE, _DECODE_OPTS, _STEP, _WRITE, _PREFILL = range(6)
+_APPEND, _DECODE, _DECODE_OPTS, _STEP, _WRITE, _PREFILL, _READ, _ROPE = range(8)
 
 
 def library_path() -> str:
@@ -144,6 +149,10 @@ def library():
     lib.bellman_probe_gather.restype = ctypes.c_int
     lib.bellman_kv_write.argtypes = [T, T, T, T, T, T, T, P]
     lib.bellman_kv_write.restype = ctypes.c_int
+    lib.bellman_kv_read.argtypes = [T, T, T, T, T, T, T, P]
+    lib.bellman_kv_read.restype = ctypes.c_int
+    lib.bellman_qk_norm_rope.argtypes = [T, T, T, T, T, T, T, T, ctypes.POINTER(RopeOpts), P]
+    lib.bellman_qk_norm_rope.restype = ctypes.c_int
     lib.bellman_prefill_attention.argtypes = [T, T, T, T, T, T, ctypes.c_float, T, P]
     lib.bellman_prefill_attention.restype = ctypes.c_int
     lib.bellman_prefill_attention_opts.argtypes = [T, T, T, T, T, T, ctypes.c_float, T,
@@ -181,7 +190,7 @@ def library():
     lib.bellman_version.argtypes = []
     lib.bellman_version.restype = ctypes.c_char_p
     for name in ("kv_append", "decode_attention", "decode_attention_noalloc", "decode_step", "kv_write",
-                 "prefill_attention"):
+                 "prefill_attention", "kv_read", "qk_norm_rope"):
         _addr[name] = ctypes.cast(getattr(lib, "bellman_" + name), P).value
     marshal = _load_marshal()
     _native = None if marshal is None else marshal.call
@@ -208,6 +217,7 @@ _DTYPES = {
     torch.float8_e4m3fn: FP8_E4M3FN,
     torch.int32: INT32,
     torch.float32: FP32,
+    torch.float4_e2m1fn_x2: FP4_E2M1,  # 4-bit pools: bytes of two codes, and scale bytes
 }
 
 
@@ -365,6 +375,40 @@ def kv_write(k_new, v_new, k_pages, v_pages, block_table, seq_lens, q_start, str
     _device_tensors(k_new, v_new, k_pages, v_pages, block_table, seq_lens, q_start)
     _check(library().bellman_kv_write(desc(k_new), desc(v_new), desc(k_pages), desc(v_pages), desc(block_table),
                                       desc(seq_lens), desc(q_start), _stream(stream)))
+
+
+def kv_read(k_pages, v_pages, block_table, seq_lens, q_start, k_out, v_out, stream=None, k_scale=None, v_scale=None):
+    """bellman_kv_read: each request's last q_start[b + 1] - q_start[b] cached
+    rows as bf16 (fp8 pools with their scales k_scale / v_scale)."""
+    if _call("kv_read", _READ, stream, 0.0, 0, k_scale, v_scale, k_pages, v_pages, block_table, seq_lens, q_start,
+             k_out, v_out):
+        return
+    _device_tensors(k_pages, v_pages, block_table, seq_lens, q_start, k_out, v_out, k_scale, v_scale)
+    _check(library().bellman_kv_read(desc(k_pages, k_scale), desc(v_pages, v_scale), desc(block_table),
+                                     desc(seq_lens), desc(q_start), desc(k_out), desc(v_out), _stream(stream)))
+
+
+def qk_norm_rope(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
+                 sections=None, interleaved=False, stream=None):
+    """bellman_qk_norm_rope: norm (where a weight is given) and rotation of
+    queries and keys, before the cache.
+
+    ``sections`` gives the frequencies each position axis turns, with
+    ``positions`` int32 [len(sections), T]; None: one axis, positions [T]."""
+    opts = RopeOpts(float(eps), float(weight_offset), int(bool(interleaved)))
+    if sections is not None:
+        if not 2 <= len(sections) <= 4:
+            raise ValueError("sections: two to four axes")
+        opts.axes = len(sections)
+        for i, n in enumerate(sections):
+            opts.sections[i] = int(n)
+    if _call("qk_norm_rope", _ROPE, stream, 0.0, ctypes.addressof(opts), None, None, q, k, q_weight, k_weight,
+             positions, inv_freq, q_out, k_out):
+        return
+    _device_tensors(q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out)
+    _check(library().bellman_qk_norm_rope(
+        desc(q), desc(k), None if q_weight is None else desc(q_weight), None if k_weight is None else desc(k_weight),
+        desc(positions), desc(inv_freq), desc(q_out), desc(k_out), ctypes.byref(opts), _stream(stream)))
 
 
 def prefill_attention(q, k_pages, v_pages, block_table, seq_lens, q_start, scale, out, stream=None,

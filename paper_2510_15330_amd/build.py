@@ -19,7 +19,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbellman.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")     # CPython extension, host only
-DEVICE_SOURCES = ["kernels.hip", "prefill.hip", "device_state.hip", "probe.hip"]
+DEVICE_SOURCES = ["kernels.hip", "prefill.hip", "rope.hip", "device_state.hip", "probe.hip"]
 HOST_SOURCES = ["bellman_api.cpp", "controller.cpp", "serve_sim.cpp"]
 SOURCES = DEVICE_SOURCES + HOST_SOURCES
 

@@ -57,7 +57,7 @@ struct Workspace {
 std::mutex g_ws_mutex;
 Workspace g_ws[kMaxDevices];
 int g_cu_count[kMaxDevices];
-int g_blocks_per_cu[kMaxDevices][2][2][5][3];  // [dev][fp8][D==128][pages per step][depth], 0 = unknown
+int g_blocks_per_cu[kMaxDevices][3][2][5][3];  // [dev][pool type][D==128][pages per step][depth], 0 = unknown
 
 int current_device(int* dev) {
     hipError_t e = hipGetDevice(dev);
@@ -128,6 +128,7 @@ int elem_size(int32_t dt) {
     switch (dt) {
         case BELLMAN_BF16: return 2;
         case BELLMAN_FP8_E4M3FN: return 1;
+        case BELLMAN_FP4_E2M1: return 1;   // two codes a byte; shapes and strides count bytes
         case BELLMAN_INT32: return 4;
         case BELLMAN_FP32: return 4;
         default: return 0;
@@ -138,6 +139,7 @@ const char* dtype_name(int32_t dt) {
     switch (dt) {
         case BELLMAN_BF16: return "bf16";
         case BELLMAN_FP8_E4M3FN: return "fp8_e4m3fn";
+        case BELLMAN_FP4_E2M1: return "fp4_e2m1";
         case BELLMAN_INT32: return "int32";
         case BELLMAN_FP32: return "fp32";
         default: return "unknown";
@@ -177,16 +179,52 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 struct PoolShape {
     int64_t num_pages;
     int H_kv, D, x;
-    bool fp8;
+    bool fp8, fp4;
+    int kv;             // kKvBf16, kKvFp8 or kKvFp4
 };
+
+// 4-bit pools: K and V [NP, H_kv, 17, D/2] bytes, contiguous.
+int check_pools4(const bellman_tensor_t* k, const bellman_tensor_t* v, PoolShape* ps) {
+    int rc;
+    if ((rc = check_tensor(k, "k_pages", 4))) return rc;
+    if ((rc = check_tensor(v, "v_pages", 4))) return rc;
+    if ((rc = check_dtype(v, "v_pages", BELLMAN_FP4_E2M1))) return rc;
+    if (k->shape[2] != kTile4Rows)
+        return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: %lld rows a tile, expected %d (16 of codes, one of scales)",
+                    (long long)k->shape[2], kTile4Rows);
+    for (int i = 0; i < 4; ++i)
+        if (v->shape[i] != k->shape[i])
+            return fail(BELLMAN_ERR_INVALID_ARG, "v_pages: dim %d is %lld, k_pages has %lld", i, (long long)v->shape[i],
+                        (long long)k->shape[i]);
+    const int64_t half = k->shape[3];
+    if (half != 32 && half != 64) return fail(BELLMAN_ERR_UNSUPPORTED, "head_dim %lld: only 64 and 128 are supported", (long long)(2 * half));
+    if (k->shape[1] < 1 || k->shape[1] > INT32_MAX) return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: %lld KV heads", (long long)k->shape[1]);
+    if (k->shape[0] < 1) return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: the pool has no pages");
+    if (k->shape[0] > INT32_MAX) return fail(BELLMAN_ERR_UNSUPPORTED, "more than 2^31-1 pages");
+    if (!is_contiguous(k)) return fail(BELLMAN_ERR_UNSUPPORTED, "k_pages: must be contiguous");
+    if (!is_contiguous(v)) return fail(BELLMAN_ERR_UNSUPPORTED, "v_pages: must be contiguous");
+    if (!aligned(k->data, 16) || !aligned(v->data, 16))
+        return fail(BELLMAN_ERR_UNSUPPORTED, "k_pages/v_pages: data must be 16-byte aligned");
+    if (k->dequant_scale || v->dequant_scale)
+        return fail(BELLMAN_ERR_INVALID_ARG, "dequant_scale is only meaningful for fp8 pools (4-bit tiles hold their scales)");
+    ps->num_pages = k->shape[0];
+    ps->H_kv = (int)k->shape[1];
+    ps->D = (int)(2 * half);
+    ps->x = 0;
+    ps->fp8 = false;
+    ps->fp4 = true;
+    ps->kv = kKvFp4;
+    return BELLMAN_OK;
+}
 
 // K [NP, H_kv, D/x, 16, x], V [NP, H_kv, D, 16], same dtype, contiguous.
 int check_pools(const bellman_tensor_t* k, const bellman_tensor_t* v, PoolShape* ps, bool need_scales) {
     int rc;
+    if (k && k->dtype == BELLMAN_FP4_E2M1) return check_pools4(k, v, ps);
     if ((rc = check_tensor(k, "k_pages", 5))) return rc;
     if ((rc = check_tensor(v, "v_pages", 4))) return rc;
     if (k->dtype != BELLMAN_BF16 && k->dtype != BELLMAN_FP8_E4M3FN)
-        return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: dtype %s, expected bf16 or fp8_e4m3fn", dtype_name(k->dtype));
+        return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: dtype %s, expected bf16, fp8_e4m3fn or fp4_e2m1", dtype_name(k->dtype));
     if (v->dtype != k->dtype)
         return fail(BELLMAN_ERR_INVALID_ARG, "v_pages: dtype %s differs from k_pages %s", dtype_name(v->dtype),
                     dtype_name(k->dtype));
@@ -219,6 +257,8 @@ int check_pools(const bellman_tensor_t* k, const bellman_tensor_t* v, PoolShape*
     ps->D = (int)D;
     ps->x = (int)x;
     ps->fp8 = fp8;
+    ps->fp4 = false;
+    ps->kv = fp8 ? kKvFp8 : kKvBf16;
     return BELLMAN_OK;
 }
 
@@ -272,7 +312,8 @@ int launch_status(const char* what) {
 int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages, const bellman_tensor_t* v_pages,
                      const bellman_tensor_t* block_table, const bellman_tensor_t* seq_lens, float scale,
                      bellman_tensor_t* out, const bellman_attn_opts_t* opts, void* stream, bool fixed,
-                     const bellman_tensor_t* k_new = nullptr, const bellman_tensor_t* v_new = nullptr) {
+                     const bellman_tensor_t* k_new = nullptr, const bellman_tensor_t* v_new = nullptr,
+                     bool check_only = false) {
     g_last_error[0] = 0;
     int rc;
     PoolShape ps;
@@ -288,14 +329,15 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     if (H_q < 1 || H_q % ps.H_kv != 0)
         return fail(BELLMAN_ERR_INVALID_ARG, "query heads %lld not a multiple of KV heads %d", (long long)H_q, ps.H_kv);
     // decode step: the new rows, as for bellman_kv_append
-    const bool step = k_new != nullptr || v_new != nullptr;
+    bool step = k_new != nullptr || v_new != nullptr;
     bool quant = false;
     if (step) {
         if ((rc = check_tensor(k_new, "k_new", 3))) return rc;
         quant = ps.fp8 && k_new->dtype == BELLMAN_BF16;
-        const int32_t row_dtype = quant ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
+        const int32_t row_dtype = quant || ps.fp4 ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
         if ((rc = check_rows(k_new, "k_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
         if ((rc = check_rows(v_new, "v_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
+        step = !ps.fp4;      // 4-bit pools: the caller makes the append's launch
     }
     const int64_t G = H_q / ps.H_kv;
     if (G > 16) return fail(BELLMAN_ERR_UNSUPPORTED, "GQA group %lld > 16", (long long)G);
@@ -316,9 +358,12 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
         if (skew_opt < -1 || skew_opt > kMaxSkew)
             return fail(BELLMAN_ERR_INVALID_ARG, "xcd_skew %d not in [-1, %d]", skew_opt, kMaxSkew);
     }
-    if (pps == 4 && !ps.fp8) return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step 4 is built for fp8 pools only");
+    if (pps == 4 && ps.kv == kKvBf16)
+        return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step 4 is built for fp8 and 4-bit pools only");
+    if (ps.fp4 && pps != 0 && pps != 4)
+        return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step %d: 4-bit pools take 4 pages a step", pps);
     const bool chosen = pps == 0 && depth == 0;   // the step is the library's choice
-    if (depth == 0) depth = ps.fp8 ? 1 : 2;
+    if (depth == 0) depth = ps.kv == kKvBf16 ? 2 : 1;
     if (B == 0) return BELLMAN_OK;
 
     int dev;
@@ -334,7 +379,7 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
         // for few pages per wave (short shares: the finer step shortens the
         // ramp and the tail; 121 against 126 us on 64 requests of 1-4k tokens,
         // while 256 requests of 6-13.5k tokens run faster with two).
-        pps = ps.fp8 ? 4 : (table_pages_per_wave < kShortSharePages ? 1 : 2);
+        pps = ps.kv != kKvBf16 ? 4 : (table_pages_per_wave < kShortSharePages ? 1 : 2);
     }
     // Short bf16 shares run one step ahead instead of two, still one wave a
     // SIMD: the pipeline fills and drains a step sooner (calls, depth 2 / 1:
@@ -345,27 +390,27 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     // shares only (64 of 50-200 13.0 / 12.9 us, 16 of 1-2k 17.6 / 16.2, 64 of
     // 1-4k 59.4 / 60.3).
     const int asked_depth = depth;
-    if (chosen && !ps.fp8 && table_pages_per_wave < (ps.D == 128 ? kShortSharePages : kShortSharePages64)) {
+    if (chosen && ps.kv == kKvBf16 && table_pages_per_wave < (ps.D == 128 ? kShortSharePages : kShortSharePages64)) {
         if (ps.D == 64) pps = 2;
         if (!step) depth = 1;               // (the step is built at depth 2)
     }
-    if (step && !attention_step_built(pps, asked_depth, ps.fp8))
+    if (step && !attention_step_built(pps, asked_depth, ps.kv))
         return fail(BELLMAN_ERR_UNSUPPORTED,
                     "decode step: built for the default steps only (bf16: 1 or 2 pages, depth 2; fp8: 4 pages, "
                     "depth 1)");
     int64_t* wave_times = opts ? opts->wave_times : nullptr;
     if (step && wave_times) return fail(BELLMAN_ERR_UNSUPPORTED, "decode step: wave_times is not built for it");
-    if (wave_times && !attention_traced(pps, asked_depth, ps.fp8, ps.D))
+    if (wave_times && !attention_traced(pps, asked_depth, ps.kv, ps.D))
         return fail(BELLMAN_ERR_UNSUPPORTED,
                     "wave_times: traced kernels are built for head_dim 128 at the default steps only");
     if (wave_times && !aligned(wave_times, 8)) return fail(BELLMAN_ERR_UNSUPPORTED, "wave_times must be 8-byte aligned");
-    int& cached = g_blocks_per_cu[dev][ps.fp8][ps.D == 128][pps][depth];
+    int& cached = g_blocks_per_cu[dev][ps.kv][ps.D == 128][pps][depth];
     if (cached == 0) {
         // one wavefront per SIMD at depth 2; at depth 1 as many as fit, up to
         // a bound: whether a third workgroup of the fp8 default step fits at
         // head_dim 64 hangs on one register of a compilation (167 or 169), and
         // it costs (512 requests with Zipf lengths 342 us against 312)
-        const int fit = attention_blocks_per_cu(pps, depth, ps.fp8, ps.D);
+        const int fit = attention_blocks_per_cu(pps, depth, ps.kv, ps.D);
         cached = depth == 2 ? 1 : std::min(fit, pps == 4 ? 2 : 4);
     }
     const int bpc = cached;
@@ -423,6 +468,7 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     }
     int32_t* err;
     if ((rc = device_error_word(dev, &err))) return rc;
+    if (check_only) return BELLMAN_OK;
 
     AttnArgs a;
     a.q = (const uint16_t*)q->data;
@@ -452,7 +498,7 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     // workgroup i on XCD i mod 8), with one and with two workgroups per CU;
     // partitioned devices keep equal shares.
     if (skew_opt == 0)
-        a.skew = g_cu_count[dev] != 256 ? 0 : wgs == 1 && !ps.fp8 ? kXcdSkew : wgs > 1 || G <= 8 ? kXcdSkew2 : 0;
+        a.skew = g_cu_count[dev] != 256 ? 0 : wgs == 1 && ps.kv == kKvBf16 ? kXcdSkew : wgs > 1 || G <= 8 ? kXcdSkew2 : 0;
     else a.skew = skew_opt < 0 ? 0 : skew_opt;
     a.err = err;
     a.cuts = (int4*)(base + off_cuts);
@@ -474,7 +520,7 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
         hipError_t e = hipEventRecord(ev0, s);
         if (e != hipSuccess) return fail(BELLMAN_ERR_HIP, "hipEventRecord: %s", hipGetErrorString(e));
     }
-    launch_attention(a, pps, depth, ps.fp8, (int)grid, s);
+    launch_attention(a, pps, depth, ps.kv, (int)grid, s);
     if ((rc = launch_status("attention"))) return rc;
     if (ev1) {
         hipError_t e = hipEventRecord(ev1, s);
@@ -559,8 +605,9 @@ int bellman_kv_append(const bellman_tensor_t* k_new, const bellman_tensor_t* v_n
     if ((rc = check_tensor(k_new, "k_new", 3))) return rc;
     const int64_t B = k_new->shape[0];
     // bf16 rows into fp8 pools are quantised with the pools' dequant scales
+    // (4-bit pools take bf16 rows only, and hold their scales)
     const bool quant = ps.fp8 && k_new->dtype == BELLMAN_BF16;
-    const int32_t row_dtype = quant ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
+    const int32_t row_dtype = quant || ps.fp4 ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
     if ((rc = check_rows(k_new, "k_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
     if ((rc = check_rows(v_new, "v_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
     if ((rc = check_block_table(block_table, B))) return rc;
@@ -597,7 +644,8 @@ int bellman_kv_append(const bellman_tensor_t* k_new, const bellman_tensor_t* v_n
     a.max_pages = (int)block_table->shape[1];
     a.elem_bytes = ps.fp8 ? 1 : 2;
     a.quant = quant ? 1 : 0;
-    launch_kv_append(a, (hipStream_t)stream);
+    if (ps.fp4) launch_kv4_append(a, (hipStream_t)stream);
+    else launch_kv_append(a, (hipStream_t)stream);
     return launch_status("kv_append");
 }
 
@@ -654,6 +702,14 @@ int bellman_decode_step(const bellman_tensor_t* k_new, const bellman_tensor_t* v
                         const bellman_attn_opts_t* opts, void* stream) {
     g_last_error[0] = 0;
     if (!k_new || !v_new) return fail(BELLMAN_ERR_INVALID_ARG, "k_new and v_new are required");
+    if (k_pages && k_pages->dtype == BELLMAN_FP4_E2M1) {
+        // the append's launch, then the attention's; nothing is written where either would be refused
+        const int rc = decode_attention(q, k_pages, v_pages, block_table, seq_lens, scale, out, opts, stream, false, k_new,
+                                        v_new, true);
+        if (rc || q->shape[0] == 0) return rc;
+        const int ra = bellman_kv_append(k_new, v_new, k_pages, v_pages, block_table, seq_lens, stream);
+        return ra ? ra : decode_attention(q, k_pages, v_pages, block_table, seq_lens, scale, out, opts, stream, false);
+    }
     return decode_attention(q, k_pages, v_pages, block_table, seq_lens, scale, out, opts, stream, false, k_new, v_new);
 }
 
@@ -672,18 +728,23 @@ int check_q_start(const bellman_tensor_t* qs, int64_t B) {
 }
 }  // namespace
 
-int bellman_kv_write(const bellman_tensor_t* k_new, const bellman_tensor_t* v_new, bellman_tensor_t* k_pages,
-                     bellman_tensor_t* v_pages, const bellman_tensor_t* block_table, bellman_tensor_t* seq_lens,
-                     const bellman_tensor_t* q_start, void* stream) {
+// The prompt write (read false: k_new, v_new into the pages) and its reverse
+// (read true: the last rows of each request into k_new, v_new, as bf16).
+static int write_or_read(bool read, const bellman_tensor_t* k_new, const bellman_tensor_t* v_new,
+                         const bellman_tensor_t* k_pages, const bellman_tensor_t* v_pages,
+                         const bellman_tensor_t* block_table, const bellman_tensor_t* seq_lens,
+                         const bellman_tensor_t* q_start, void* stream) {
     g_last_error[0] = 0;
     int rc;
     PoolShape ps;
-    if ((rc = check_pools(k_pages, v_pages, &ps, false))) return rc;
-    if ((rc = check_tensor(k_new, "k_new", 3))) return rc;
+    const char* kname = read ? "k_out" : "k_new";
+    const char* vname = read ? "v_out" : "v_new";
+    if ((rc = check_pools(k_pages, v_pages, &ps, read))) return rc;
+    if ((rc = check_tensor(k_new, kname, 3))) return rc;
     const int64_t T = k_new->shape[0];
-    const size_t eb = ps.fp8 ? 1 : 2;
-    if ((rc = check_rows(k_new, "k_new", k_pages->dtype, T, ps.H_kv, ps.D, 16))) return rc;
-    if ((rc = check_rows(v_new, "v_new", k_pages->dtype, T, ps.H_kv, ps.D, 16))) return rc;
+    const int32_t row_dtype = read || ps.fp4 ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
+    if ((rc = check_rows(k_new, kname, row_dtype, T, ps.H_kv, ps.D, 16))) return rc;
+    if ((rc = check_rows(v_new, vname, row_dtype, T, ps.H_kv, ps.D, 16))) return rc;
     if ((rc = check_seq_lens(seq_lens, seq_lens ? seq_lens->shape[0] : 0))) return rc;
     const int64_t B = seq_lens->shape[0];
     if ((rc = check_block_table(block_table, B))) return rc;
@@ -720,9 +781,131 @@ int bellman_kv_write(const bellman_tensor_t* k_new, const bellman_tensor_t* v_ne
     a.H_kv = ps.H_kv;
     a.D = ps.D;
     a.max_pages = (int)block_table->shape[1];
-    a.elem_bytes = (int)eb;
-    launch_kv_write(a, (int32_t*)(base + kWsHeader), (hipStream_t)stream);
-    return launch_status("kv_write");
+    a.elem_bytes = ps.kv == kKvBf16 ? 2 : 1;
+    a.kv = ps.kv;
+    a.k_scale = k_pages->dequant_scale;
+    a.v_scale = v_pages->dequant_scale;
+    if (read) launch_kv_read(a, (int32_t*)(base + kWsHeader), (hipStream_t)stream);
+    else launch_kv_write(a, (int32_t*)(base + kWsHeader), (hipStream_t)stream);
+    return launch_status(read ? "kv_read" : "kv_write");
+}
+
+int bellman_kv_write(const bellman_tensor_t* k_new, const bellman_tensor_t* v_new, bellman_tensor_t* k_pages,
+                     bellman_tensor_t* v_pages, const bellman_tensor_t* block_table, bellman_tensor_t* seq_lens,
+                     const bellman_tensor_t* q_start, void* stream) {
+    return write_or_read(false, k_new, v_new, k_pages, v_pages, block_table, seq_lens, q_start, stream);
+}
+
+int bellman_kv_read(const bellman_tensor_t* k_pages, const bellman_tensor_t* v_pages,
+                    const bellman_tensor_t* block_table, const bellman_tensor_t* seq_lens,
+                    const bellman_tensor_t* q_start, bellman_tensor_t* k_out, bellman_tensor_t* v_out, void* stream) {
+    return write_or_read(true, k_out, v_out, k_pages, v_pages, block_table, seq_lens, q_start, stream);
+}
+
+// ------------------------------------------------------ norm and rotation --
+
+namespace {
+// [D] of bf16 or fp32, contiguous; null descriptor: none
+int check_weight(const bellman_tensor_t* t, const char* name, int64_t D) {
+    if (!t) return BELLMAN_OK;
+    int rc;
+    if ((rc = check_tensor(t, name, 1))) return rc;
+    if (t->dtype != BELLMAN_BF16 && t->dtype != BELLMAN_FP32)
+        return fail(BELLMAN_ERR_INVALID_ARG, "%s: dtype %s, expected bf16 or fp32", name, dtype_name(t->dtype));
+    if (t->shape[0] != D)
+        return fail(BELLMAN_ERR_INVALID_ARG, "%s: %lld entries, expected %lld", name, (long long)t->shape[0], (long long)D);
+    if (t->stride[0] != 1) return fail(BELLMAN_ERR_UNSUPPORTED, "%s: must be contiguous", name);
+    if (!aligned(t->data, elem_size(t->dtype))) return fail(BELLMAN_ERR_UNSUPPORTED, "%s: misaligned data", name);
+    return BELLMAN_OK;
+}
+}  // namespace
+
+int bellman_qk_norm_rope(const bellman_tensor_t* q, const bellman_tensor_t* k, const bellman_tensor_t* q_weight,
+                         const bellman_tensor_t* k_weight, const bellman_tensor_t* positions,
+                         const bellman_tensor_t* inv_freq, bellman_tensor_t* q_out, bellman_tensor_t* k_out,
+                         const bellman_rope_opts_t* opts, void* stream) {
+    g_last_error[0] = 0;
+    int rc;
+    if ((rc = check_tensor(q, "q", 3))) return rc;
+    if ((rc = check_tensor(k, "k", 3))) return rc;
+    const int64_t T = q->shape[0], H_q = q->shape[1], H_kv = k->shape[1], D = q->shape[2];
+    if (D != 64 && D != 128) return fail(BELLMAN_ERR_UNSUPPORTED, "head_dim %lld: only 64 and 128 are supported", (long long)D);
+    if ((rc = check_rows(q, "q", BELLMAN_BF16, T, H_q, D, 16))) return rc;
+    if ((rc = check_rows(k, "k", BELLMAN_BF16, T, H_kv, D, 16))) return rc;
+    if ((rc = check_rows(q_out, "q_out", BELLMAN_BF16, T, H_q, D, 16))) return rc;
+    if ((rc = check_rows(k_out, "k_out", BELLMAN_BF16, T, H_kv, D, 16))) return rc;
+    if ((rc = check_weight(q_weight, "q_weight", D))) return rc;
+    if ((rc = check_weight(k_weight, "k_weight", D))) return rc;
+    if ((rc = check_tensor(inv_freq, "inv_freq", 1))) return rc;
+    if ((rc = check_dtype(inv_freq, "inv_freq", BELLMAN_FP32))) return rc;
+    const int64_t half = inv_freq->shape[0];
+    if (half < 1 || 2 * half > D)
+        return fail(BELLMAN_ERR_INVALID_ARG, "inv_freq: %lld frequencies for head_dim %lld", (long long)half, (long long)D);
+    if (half % 8) return fail(BELLMAN_ERR_UNSUPPORTED, "inv_freq: %lld frequencies, not a multiple of 8", (long long)half);
+    if (half > 1 && inv_freq->stride[0] != 1) return fail(BELLMAN_ERR_UNSUPPORTED, "inv_freq: must be contiguous");
+    if (!aligned(inv_freq->data, 4)) return fail(BELLMAN_ERR_UNSUPPORTED, "inv_freq: misaligned data");
+    const bellman_rope_opts_t defaults = {1e-6f, 0.f, 0, 1, {0, 0, 0, 0}};
+    const bellman_rope_opts_t& o = opts ? *opts : defaults;
+    const int axes = o.axes == 0 ? 1 : o.axes;
+    if (axes < 1 || axes > 4) return fail(BELLMAN_ERR_UNSUPPORTED, "%d position axes: 1 to 4 are supported", o.axes);
+    if (o.interleaved != 0 && o.interleaved != 1) return fail(BELLMAN_ERR_INVALID_ARG, "interleaved %d not in {0, 1}", o.interleaved);
+    if (!isfinite(o.eps) || o.eps < 0.f) return fail(BELLMAN_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (!isfinite(o.weight_offset)) return fail(BELLMAN_ERR_INVALID_ARG, "weight_offset must be finite");
+    if ((rc = check_tensor(positions, "positions", axes == 1 ? 1 : 2))) return rc;
+    if ((rc = check_dtype(positions, "positions", BELLMAN_INT32))) return rc;
+    const int pd = axes == 1 ? 0 : 1;
+    if ((axes > 1 && positions->shape[0] != axes) || positions->shape[pd] != T)
+        return fail(BELLMAN_ERR_INVALID_ARG, "positions: %lld x %lld, expected %d axes of %lld tokens",
+                    (long long)(axes > 1 ? positions->shape[0] : 1), (long long)positions->shape[pd], axes, (long long)T);
+    if (T > 1 && positions->stride[pd] != 1) return fail(BELLMAN_ERR_UNSUPPORTED, "positions: tokens must be contiguous");
+    if (!aligned(positions->data, 4)) return fail(BELLMAN_ERR_UNSUPPORTED, "positions: misaligned data");
+    if (H_q < 1 || H_kv < 1) return fail(BELLMAN_ERR_INVALID_ARG, "q and k need a head each");
+    if (H_q > 65535 || H_kv > 65535) return fail(BELLMAN_ERR_UNSUPPORTED, "more than 65535 heads");
+    if (T > INT32_MAX / 2) return fail(BELLMAN_ERR_UNSUPPORTED, "too many tokens");
+    RopeArgs a;
+    // axis x turns sections[x] frequencies, in order
+    int64_t sum = 0;
+    for (int x = 0; x < 4; ++x) {
+        if (axes > 1 && x < axes) {
+            if (o.sections[x] < 0) return fail(BELLMAN_ERR_INVALID_ARG, "sections[%d] = %d < 0", x, o.sections[x]);
+            sum += o.sections[x];
+        }
+        if (x < 3) a.cut[x] = axes == 1 || x >= axes - 1 ? (int)half : (int)std::min<int64_t>(sum, half);
+    }
+    if (axes > 1 && sum != half)
+        return fail(BELLMAN_ERR_INVALID_ARG, "sections sum to %lld, inv_freq has %lld frequencies", (long long)sum, (long long)half);
+    if (T == 0) return BELLMAN_OK;
+    a.q = (const uint16_t*)q->data;
+    a.k = (const uint16_t*)k->data;
+    a.q_out = (uint16_t*)q_out->data;
+    a.k_out = (uint16_t*)k_out->data;
+    a.q_st = q->stride[0];
+    a.q_sh = q->stride[1];
+    a.k_st = k->stride[0];
+    a.k_sh = k->stride[1];
+    a.qo_st = q_out->stride[0];
+    a.qo_sh = q_out->stride[1];
+    a.ko_st = k_out->stride[0];
+    a.ko_sh = k_out->stride[1];
+    a.q_weight = q_weight ? q_weight->data : nullptr;
+    a.k_weight = k_weight ? k_weight->data : nullptr;
+    a.qw_fp32 = q_weight && q_weight->dtype == BELLMAN_FP32;
+    a.kw_fp32 = k_weight && k_weight->dtype == BELLMAN_FP32;
+    a.positions = (const int32_t*)positions->data;
+    a.pos_stride = axes == 1 ? 0 : positions->stride[0];
+    a.inv_freq = (const float*)inv_freq->data;
+    a.eps = o.eps;
+    a.offset = o.weight_offset;
+    a.T = (int)T;
+    a.H_q = (int)H_q;
+    a.H_kv = (int)H_kv;
+    a.D = (int)D;
+    a.R = (int)(2 * half);
+    a.axes = axes;
+    a.interleaved = o.interleaved;
+    a.chunks = 1;
+    launch_qk_norm_rope(a, (hipStream_t)stream);
+    return launch_status("qk_norm_rope");
 }
 
 int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
@@ -773,7 +956,7 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     // 17 against 11 us.  From two rounds on the hardware's own balance is left
     // to do it (2048 tiles, four rounds: the same uncut).  A table of no more
     // keys than one unit takes is never cut, and needs no merge launch.
-    PrefillArgs a;
+    PrefillArgs a = {};
     const int64_t rows = T * (H_q / ps.H_kv);
     a.max_tiles = (rows / kPrefillRows + B) * ps.H_kv;
     a.slots = 2 * g_cu_count[dev];
@@ -788,7 +971,9 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     const size_t off_req = off_steps + align256(planned && !ps.fp8 ? (size_t)(B + 1) * 4 : 0);
     const size_t off_exp = off_req + align256(planned && !ps.fp8 ? max_steps * 4 : 0);
     const size_t off_copy = off_exp + align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4);
-    const size_t off_ml = off_copy + align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4 * page_head_bytes);
+    const size_t copy_bytes = align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4 * page_head_bytes);
+    const size_t off_kcopy = off_copy + copy_bytes;      // 4-bit pools: the keys' copy
+    const size_t off_ml = off_kcopy + (ps.fp4 ? copy_bytes : 0);
     const size_t piece_rows = a.split ? (size_t)a.max_units * kPrefillRows : 0;
     const size_t off_o = off_ml + align256(piece_rows * sizeof(float2));
     const size_t total = off_o + align256(piece_rows * ps.D * sizeof(float));
@@ -845,6 +1030,7 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     a.step_req = (int32_t*)(base + off_req);
     a.vexp = (int32_t*)(base + off_exp);
     a.vcopy = (uint16_t*)(base + off_copy);
+    a.kcopy = ps.fp4 ? (uint16_t*)(base + off_kcopy) : nullptr;
     // a workgroup for every (step, head) tile of B x maxP pages at most once,
     // and at most 4096
     a.vgrid = (int)std::max<int64_t>(1, std::min<int64_t>(4096, (int64_t)max_steps * ps.H_kv));

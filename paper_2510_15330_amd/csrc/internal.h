@@ -10,6 +10,11 @@ namespace bellman {
 
 constexpr int kPage = 16;           // tokens per KV page
 constexpr int kWaveSize = 64;       // CDNA wavefront
+// The pools' element types, and the rows of D / 2 bytes of a 4-bit tile (16 of
+// codes, one of scales).
+constexpr int kKvBf16 = 0, kKvFp8 = 1, kKvFp4 = 2;
+constexpr int kTile4Rows = 17;
+
 constexpr int kAttnBlock = 256;     // threads per attention workgroup (4 independent waves)
 
 // Device error word bits (also documented in bellman.h).
@@ -87,10 +92,10 @@ struct AttnArgs {
     int32_t* lens_rw;    // seq_lens, advanced by the merge pass
 };
 
-// Prompt KV write (prefill.hip).
+// Prompt KV write, and the read back of cached rows (prefill.hip).
 struct WriteArgs {
-    const void* k_new;   // [T, H_kv, D] pool element type
-    const void* v_new;
+    const void* k_new;   // [T, H_kv, D] pool element type (bf16 for 4-bit pools);
+    const void* v_new;   // a read writes its bf16 rows here
     int64_t k_st, k_sh, v_st, v_sh;   // row strides (elements)
     void* k_pages;
     void* v_pages;
@@ -101,6 +106,9 @@ struct WriteArgs {
     int32_t* err;
     int64_t num_pages;
     int B, T, H_kv, D, max_pages, elem_bytes;
+    int kv;                // the pools' type
+    const float* k_scale;  // reading fp8 pools only: fp32 [B, H_kv]
+    const float* v_scale;
 };
 
 // Prompt (prefill) attention over the paged cache (prefill.hip).
@@ -139,21 +147,44 @@ struct PrefillArgs {
     int32_t* step_req;     // [B * ceil(maxP / 4)]: the request of each copied step (B > 64)
     int32_t* vexp;         // [copied steps, H_kv]: the exponent of the step's scale
     uint16_t* vcopy;       // [copied steps, H_kv, 4 pages, D, 16] fp16
+    uint16_t* kcopy;       // 4-bit pools: the keys as bf16, [copied steps, H_kv, 4 pages, D/8, 16, 8]; else null
     int vgrid;             // workgroups of the copy
 };
+
+// Norm and rotation of queries and keys (rope.hip).
+struct RopeArgs {
+    const uint16_t* q;   // bf16 [T, H_q, D]
+    const uint16_t* k;   // bf16 [T, H_kv, D]
+    uint16_t* q_out;
+    uint16_t* k_out;
+    int64_t q_st, q_sh, k_st, k_sh, qo_st, qo_sh, ko_st, ko_sh;   // strides (elements)
+    const void* q_weight;      // [D] bf16 or fp32, null: no norm
+    const void* k_weight;
+    const int32_t* positions;  // [axes, T]
+    int64_t pos_stride;
+    const float* inv_freq;     // [R / 2]
+    float eps, offset;
+    int T, H_q, H_kv, D, R;
+    int axes, cut[3];          // frequency f turns by axis: the first x with f < cut[x], else 3
+    int qw_fp32, kw_fp32, interleaved;
+    int chunks;                // waves a token (set by the launcher)
+};
+void launch_qk_norm_rope(const RopeArgs& a, hipStream_t s);
 
 // Launchers (kernels.hip).  They only enqueue; errors come back through
 // hipGetLastError in the caller.
 void launch_kv_append(const AppendArgs& a, hipStream_t s);
-void launch_attention(const AttnArgs& a, int pages_per_step, int depth, bool fp8, int grid, hipStream_t s);
+void launch_attention(const AttnArgs& a, int pages_per_step, int depth, int kv, int grid, hipStream_t s);
 // Whether the attention kernel variant has a traced twin (wave_times).
-bool attention_traced(int pages_per_step, int depth, bool fp8, int D);
+bool attention_traced(int pages_per_step, int depth, int kv, int D);
 // Whether the attention kernel variant has a decode-step twin (k_new set).
-bool attention_step_built(int pages_per_step, int depth, bool fp8);
+bool attention_step_built(int pages_per_step, int depth, int kv);
 // Resident workgroups per CU of the attention kernel variant (occupancy).
-int attention_blocks_per_cu(int pages_per_step, int depth, bool fp8, int D);
+int attention_blocks_per_cu(int pages_per_step, int depth, int kv, int D);
 void launch_merge(const AttnArgs& a, hipStream_t s);
-// Prefill launchers (prefill.hip).
+// Prefill launchers (prefill.hip), the append into 4-bit pools among them.
+void launch_kv4_append(const AppendArgs& a, hipStream_t s);
+void launch_kv_read(const WriteArgs& a, int32_t* page_start, hipStream_t s);
 void launch_kv_write(const WriteArgs& a, int32_t* page_start, hipStream_t s);
 // The prompt attention's planning (B > 64) and, over bf16 pools, the fp16
 // value copy; then the attention kernel itself and the key-split merge.

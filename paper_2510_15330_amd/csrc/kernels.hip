@@ -691,6 +691,185 @@ __device__ __forceinline__ void fp8_step(AttnState<D>& st, const PageK<D, true> 
     }
 }
 
+// ------------------------------------------------- 4-bit pages on MFMA ---
+// A page of one head is a tile of 17 D / 2 bytes: 8 D bytes of e2m1 codes and
+// D / 2 E8M0 scales, one for every 32 dims of a token (bellman.h).
+//
+// QK: the matrix cores take K as it lies.  In v_mfma_scale_f32_16x16x128_f8f6f4
+// with A in e2m1, lane (qg, n) supplies row n at k = 32 qg .. 32 qg + 31 with
+// one E8M0 scale: slot n's block qg, 16 bytes and a scale byte of the tile.  B
+// in e4m3 takes k = 16 qg + 0..15 and 64 + 16 qg + 0..15 from lane (qg, n): the
+// order of the query terms hi + lo that the fp8 pools use (every bf16 within
+// 2^-14 of its row's largest is exact in the two).  At head_dim 64 a product
+// holds two pages: lane groups 0, 1 (k < 64) the even one, groups 2, 3 the odd
+// one, and the query terms lie in the lower or the upper k half.
+//
+// PV: codes widen exactly to bf16 (A, 16 dims x 32 tokens of a page pair).  The
+// scale of a value depends on its token and 32-dim block, so it goes into the
+// weights: the product of block b takes p 2^(s - 127), as a sum of two bf16 (hi
+// truncated, lo the remainder: 2^-14 relative).  Weights are held 2^127 times
+// as large (their reference is 127 below the running max), so a scaled
+// weight's bf16 bits are the weight's less (254 - s) << 7, one saturating 16-bit
+// subtraction for two values; what falls below 2^-126 becomes 0 or below
+// 2^-126.  All lanes of a group read the same 16 scale bytes of a page.
+template <int D, int PP>
+struct Page4 {
+    static constexpr int NK = D == 128 ? PP : PP / 2;   // 16-byte K loads a lane
+    using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
+    u32x4 k[NK];
+    uint32_t ks[NK];      // the scale byte of k
+    VT v[PP];             // dword b: tiles 2b, 2b + 1 (dims 32 b + n, 32 b + 16 + n), slots 4qg..4qg+3
+    VT vs[PP];            // dword b: the scales of block b, slots 4qg..4qg+3
+    uint32_t chk;         // page qg: dword n (head_dim 64: n mod 8) of its V scales
+};
+
+// The query terms as B operands: [0] (and at head_dim 64 [1], moved to the
+// upper k half for the odd pages).
+template <int D>
+struct Q4 {
+    i32x8 hi[D == 128 ? 1 : 2], lo[D == 128 ? 1 : 2];
+    int s_hi, s_lo;
+};
+template <int D>
+__device__ __forceinline__ void q_to_fp4(const bf16x8 (&bq)[D / 32], Q4<D>& q4) {
+    Q8 q8;
+    q_to_fp8<D>(bq, q8);
+    q4.hi[0] = q8.hi;
+    q4.lo[0] = q8.lo;
+    if constexpr (D == 64) {
+        q4.hi[1] = i32x8{0, 0, 0, 0, q8.hi[0], q8.hi[1], q8.hi[2], q8.hi[3]};
+        q4.lo[1] = i32x8{0, 0, 0, 0, q8.lo[0], q8.lo[1], q8.lo[2], q8.lo[3]};
+    }
+    q4.s_hi = q8.s_hi;
+    q4.s_lo = q8.s_lo;
+}
+
+__device__ __forceinline__ f32x4 mfma_f4(const u32x4& a, int scale_a, const i32x8& b, int scale_b, f32x4 c) {
+    const i32x8 aw = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(aw, b, c, 4 /* e2m1 */, 0 /* e4m3 */, 0, scale_a, 0,
+                                                            scale_b);
+}
+
+// Byte BYTE of w (two e2m1 codes) -> two bf16.
+template <int BYTE>
+__device__ __forceinline__ uint32_t fp4x2_to_bf16x2(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, BYTE));
+}
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+// Two bf16 weights less `sub`, down to 0.
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t p, uint32_t sub) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, p),
+                                                                      __builtin_bit_cast(u16x2, sub)));
+}
+
+constexpr float kRef4 = 127.f;                 // the weights' reference below the max, log2
+constexpr uint32_t kDenorm127 = 0x00400000u;   // 2^-127
+
+// One step of PP = 4 pages: nv[i] slots of page i count, full: all do.
+template <int D, int PP>
+__device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, const Q4<D>& q4, float sl,
+                                         const int (&nv)[PP], int qg, int n, bool full) {
+    static_assert(PP == 4, "four pages, one a lane group in the scale check");
+    constexpr int NT = D / 16, NB = D / 32;
+    if constexpr (D == 64) {
+        // a dead slot's scale may be a NaN, which would reach the other page's
+        // sums through its zero query terms
+        if (!full) {
+#pragma unroll
+            for (int j = 0; j < PP / 2; ++j) {
+                const int live = qg < 2 ? nv[2 * j] : nv[2 * j + 1];
+                if (n >= live) pg.ks[j] = kE8M0One;
+            }
+        }
+    }
+    float x[4 * PP];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+        constexpr bool kPair = D == 64;
+        const int j = kPair ? i / 2 : i, h = kPair ? i % 2 : 0;
+        f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
+        s4 = mfma_f4(pg.k[j], (int)pg.ks[j], q4.hi[h], q4.s_hi, s4);
+        s4 = mfma_f4(pg.k[j], (int)pg.ks[j], q4.lo[h], q4.s_lo, s4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[4 * i + r] = s4[r] * sl;
+    }
+    uint32_t chk = pg.chk;
+    if (!full) {
+#pragma unroll
+        for (int i = 0; i < PP; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[4 * i + r] = (4 * qg + r < nv[i]) ? x[4 * i + r] : -INFINITY;
+        const int k = (qg == 0 ? nv[0] : qg == 1 ? nv[1] : qg == 2 ? nv[2] : nv[3]) - 4 * (D == 128 ? n >> 2 : (n & 7) >> 1);
+        chk &= k >= 4 ? 0xffffffffu : (k <= 0 ? 0u : (1u << (8 * k)) - 1u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * PP; ++i) mx = fmaxf(mx, x[i]);
+    mx = group_max4(mx);
+    const float m_new = fmaxf(st.m, mx - kRef4);
+    if (__any(m_new > st.m)) {
+        const float alpha = fast_exp2(st.m - m_new);
+        st.l *= alpha;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) st.o[t] *= alpha;
+        st.m = m_new;
+    }
+    // a NaN block of V (scale 255) makes its 32 dims NaN, whatever its weight
+    const uint32_t inv = ~chk;
+    const bool nan_byte = ((inv - 0x01010101u) & ~inv & 0x80808080u) != 0u;
+    if (__any(nan_byte)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            if (__any(nan_byte && (n & (NB - 1)) == b)) {
+                st.o[2 * b] = f32x4{NAN, NAN, NAN, NAN};
+                st.o[2 * b + 1] = f32x4{NAN, NAN, NAN, NAN};
+            }
+    }
+    uint32_t ph[2 * PP], pl[2 * PP];
+    float psum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * PP; i += 2) {
+        const float p0 = fast_exp2(x[i] - st.m), p1 = fast_exp2(x[i + 1] - st.m);
+        psum = __builtin_fmaf(p0, __uint_as_float(kDenorm127), psum);
+        psum = __builtin_fmaf(p1, __uint_as_float(kDenorm127), psum);
+        const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+        const float r0 = p0 - __uint_as_float(u0 & 0xffff0000u);
+        const float r1 = p1 - __uint_as_float(u1 & 0xffff0000u);
+        ph[i / 2] = pack_hi16(u0, u1);
+        pl[i / 2] = pack_hi16(__float_as_uint(r0), __float_as_uint(r1));
+    }
+    st.l += psum;
+#pragma unroll
+    for (int j = 0; j < PP / 2; ++j)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            u32x4 bh, bl;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                // (254 - s) << 7 of the four slots (a 255 borrows from its
+                // neighbours: the block is NaN already)
+                const uint32_t y = 0xfefefefeu - pg.vs[2 * j + e][b];
+                const uint32_t s01 = __builtin_amdgcn_perm(0u, y, 0x010c000cu) >> 1;
+                const uint32_t s23 = __builtin_amdgcn_perm(0u, y, 0x030c020cu) >> 1;
+                bh[2 * e] = scaled_pair(ph[4 * j + 2 * e], s01);
+                bh[2 * e + 1] = scaled_pair(ph[4 * j + 2 * e + 1], s23);
+                bl[2 * e] = scaled_pair(pl[4 * j + 2 * e], s01);
+                bl[2 * e + 1] = scaled_pair(pl[4 * j + 2 * e + 1], s23);
+            }
+            const bf16x8 bph = __builtin_bit_cast(bf16x8, bh), bpl = __builtin_bit_cast(bf16x8, bl);
+            const uint32_t w0 = pg.v[2 * j][b], w1 = pg.v[2 * j + 1][b];
+            const bf16x8 a0 = __builtin_bit_cast(bf16x8, u32x4{fp4x2_to_bf16x2<0>(w0), fp4x2_to_bf16x2<1>(w0),
+                                                               fp4x2_to_bf16x2<0>(w1), fp4x2_to_bf16x2<1>(w1)});
+            const bf16x8 a1 = __builtin_bit_cast(bf16x8, u32x4{fp4x2_to_bf16x2<2>(w0), fp4x2_to_bf16x2<3>(w0),
+                                                               fp4x2_to_bf16x2<2>(w1), fp4x2_to_bf16x2<3>(w1)});
+            st.o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, bph, st.o[2 * b], 0, 0, 0);
+            st.o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, bph, st.o[2 * b + 1], 0, 0, 0);
+            st.o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, bpl, st.o[2 * b], 0, 0, 0);
+            st.o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, bpl, st.o[2 * b + 1], 0, 0, 0);
+        }
+}
+
 // Mark loaded registers as read.  A step reads some of its loads only on some
 // paths (the query only at a segment change, the second page only when the
 // step has one); a register whose load was never waited for on the path taken
@@ -857,9 +1036,11 @@ constexpr int kHwRegHwId = 4 | (31 << 11);     // HW_ID, bits 31:0
 // real-time clock (100 MHz) when it starts and when it has written its last
 // result, and (XCD id << 32) | HW_ID: a timing record, not a change of the
 // computation.
-template <int D, bool FP8, int PP, int DEPTH, bool TRACE, bool STEP>
+template <int D, int KV, int PP, int DEPTH, bool TRACE, bool STEP>
 __global__ void __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(DEPTH == 1 ? 2 : 1, DEPTH == 1 ? 2 : 1)))
 attn_mfma_kernel(AttnArgs a) {
+    constexpr bool FP8 = KV == kKvFp8, FP4 = KV == kKvFp4;
+    static_assert(!FP4 || !STEP, "4-bit pools: the step makes the append's launch");
     constexpr int NT = D / 16;
     constexpr int KS = D / 32;
     constexpr int EB = FP8 ? 1 : 2;
@@ -978,7 +1159,7 @@ attn_mfma_kernel(AttnArgs a) {
         }
     }
 
-    const size_t tile_bytes = (size_t)D * kPage * EB;
+    const size_t tile_bytes = FP4 ? (size_t)kTile4Rows * D / 2 : (size_t)D * kPage * EB;
     const size_t page_stride = (size_t)a.H_kv * tile_bytes;
     const bool hv = n < a.G;
 
@@ -1084,7 +1265,7 @@ attn_mfma_kernel(AttnArgs a) {
         const uint16_t* qrow = a.q + (int64_t)c.b * a.q_sb + (int64_t)(c.g * a.G + min(n, a.G - 1)) * a.q_sh;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            const int dim0 = FP8 ? 16 * (qg + 4 * (j >> 1)) + 8 * (j & 1) : 8 * (4 * j + qg);
+            const int dim0 = FP8 || FP4 ? 16 * (qg + 4 * (j >> 1)) + 8 * (j & 1) : 8 * (4 * j + qg);
             bq[j] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + dim0));
         }
     };
@@ -1117,6 +1298,46 @@ attn_mfma_kernel(AttnArgs a) {
             const int pl = (unsigned)btv < (unsigned)a.num_pages ? btv : 0;
             load_v_rows<D>(rv, (const char*)a.v_pages + (size_t)pl * page_stride + (size_t)c.g * tile_bytes, n);
         }
+    };
+
+    auto kv4_load = [&](const Cursor& c, int btv, Page4<D, 4>& r, bool& bad) {
+        bad = false;
+        size_t off[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int pg = __builtin_amdgcn_readlane(btv, i);
+            if ((unsigned)pg >= (unsigned)a.num_pages) {
+                pg = 0;
+                bad = true;
+                bad_pages = 1;
+            }
+            off[i] = (size_t)pg * page_stride + (size_t)c.g * tile_bytes;
+        }
+        const char* kp = (const char*)a.k_pages;
+        const char* vp = (const char*)a.v_pages;
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r.k[i] = ld_stream<u32x4>(kp + off[i] + (size_t)(lane * 16));
+                r.ks[i] = ld_stream<uint8_t>(kp + off[i] + (size_t)(8 * D + lane));
+            }
+        } else {
+            // lane groups 0, 1: the pair's first page; 2, 3: its second
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const char* tile = kp + (lane < 32 ? off[2 * j] : off[2 * j + 1]);
+                r.k[j] = ld_stream<u32x4>(tile + (size_t)((lane & 31) * 16));
+                r.ks[j] = ld_stream<uint8_t>(tile + (size_t)(8 * D + (lane & 31)));
+            }
+        }
+        using VT = typename Page4<D, 4>::VT;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r.v[i] = ld_stream<VT>(vp + off[i] + (size_t)(lane * (D / 8)));
+            r.vs[i] = ld_stream<VT>(vp + off[i] + (size_t)(8 * D + qg * (D / 8)));
+        }
+        const size_t own = qg == 0 ? off[0] : qg == 1 ? off[1] : qg == 2 ? off[2] : off[3];
+        r.chk = ld_stream<uint32_t>(vp + own + (size_t)(8 * D + 4 * (n & (D / 8 - 1))));
     };
 
     // m starts at the lowest finite value: scores of -inf alone weigh nothing
@@ -1175,6 +1396,7 @@ attn_mfma_kernel(AttnArgs a) {
     // steps stay in flight.
     PageK<D, FP8> kb[DEPTH + 1][PP];
     PageV<D, FP8> vb[DEPTH + 1][PP];
+    Page4<D, 4> pb[DEPTH + 1];    // 4-bit pools: K, V and scales
     bf16x8 qb[DEPTH + 1][KS];
     float scb[DEPTH + 1];
     bool badb[DEPTH + 1];
@@ -1190,10 +1412,12 @@ attn_mfma_kernel(AttnArgs a) {
         q_load(cur[j], qb[j]);
         scb[j] = 0.f;
         if constexpr (FP8) scb[j] = scale_load(cur[j]);
-        kv_load(cur[j], bts[j], kb[j], vb[j], badb[j]);
+        if constexpr (FP4) kv4_load(cur[j], bts[j], pb[j], badb[j]);
+        else kv_load(cur[j], bts[j], kb[j], vb[j], badb[j]);
     }
     int btn = bts[DEPTH];
     Q8 q8;                 // fp8 only: query rows of (q8_b, q8_g) as fp8 operands
+    Q4<D> q4;              // 4-bit pools: the same
     int q8_b = -1, q8_g = -1;
 
     auto step = [&](auto slot) {
@@ -1202,9 +1426,10 @@ attn_mfma_kernel(AttnArgs a) {
         const int btT = bt_load(cur[DEPTH + 1]);
         q_load(cur[DEPTH], qb[ld_]);
         if constexpr (FP8) scb[ld_] = scale_load(cur[DEPTH]);
-        kv_load(cur[DEPTH], btn, kb[ld_], vb[ld_], badb[ld_]);
+        if constexpr (FP4) kv4_load(cur[DEPTH], btn, pb[ld_], badb[ld_]);
+        else kv_load(cur[DEPTH], btn, kb[ld_], vb[ld_], badb[ld_]);
         btn = btT;
-        if constexpr (FP8 && DEPTH > 1) consume(qb[sc_]);
+        if constexpr ((FP8 || FP4) && DEPTH > 1) consume(qb[sc_]);
 
         const Cursor& C = cur[0];
         float sl = a.scale_log2, vs = 1.f;
@@ -1213,7 +1438,17 @@ attn_mfma_kernel(AttnArgs a) {
             vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scb[sc_]), 32));
         }
         seg_bad = seg_bad || badb[sc_];
-        if constexpr (FP8) {
+        if constexpr (FP4) {
+            if (C.b != q8_b || C.g != q8_g) {
+                q_to_fp4<D>(qb[sc_], q4);
+                q8_b = C.b;
+                q8_g = C.g;
+            }
+            int nv[PP];
+#pragma unroll
+            for (int i = 0; i < PP; ++i) nv[i] = (i == 0 || C.len > i) ? min(kPage, C.L - (C.p + i) * kPage) : 0;
+            fp4_step<D, PP>(st, pb[sc_], q4, sl, nv, qg, n, C.len == PP && C.L >= (C.p + PP) * kPage);
+        } else if constexpr (FP8) {
             if (C.b != q8_b || C.g != q8_g) {  // new (request, head): convert its query rows
                 q_to_fp8<D>(qb[sc_], q8);
                 q8_b = C.b;
@@ -1501,36 +1736,38 @@ void launch_kv_append(const AppendArgs& a, hipStream_t s) {
 // The shapes built with a traced twin: head_dim 128 at the library's default
 // steps (bf16: one or two pages, depth 2, or one page, depth 1; fp8: four
 // pages, depth 1).
-template <int D, bool FP8, int PP, int DEPTH>
-constexpr bool kTraced = D == 128 && (FP8 ? (PP == 4 && DEPTH == 1) : (PP <= 2 && DEPTH == 2) || (PP == 1 && DEPTH == 1));
+template <int D, int KV, int PP, int DEPTH>
+constexpr bool kTraced = D == 128 && (KV == kKvFp8    ? (PP == 4 && DEPTH == 1)
+                                      : KV == kKvBf16 ? (PP <= 2 && DEPTH == 2) || (PP == 1 && DEPTH == 1)
+                                                      : false);
 
 // The shapes built with a decode-step twin (the append fused in): the
 // library's default steps, both head sizes.
-template <bool FP8, int PP, int DEPTH>
-constexpr bool kStepBuilt = FP8 ? (PP == 4 && DEPTH == 1) : (PP <= 2 && DEPTH == 2);
+template <int KV, int PP, int DEPTH>
+constexpr bool kStepBuilt = KV == kKvFp8 ? (PP == 4 && DEPTH == 1) : KV == kKvBf16 ? (PP <= 2 && DEPTH == 2) : false;
 
-template <int D, bool FP8, int PP, int DEPTH>
+template <int D, int KV, int PP, int DEPTH>
 struct Variant {
     static void launch(const AttnArgs& a, int grid, hipStream_t s) {
         if (a.k_new != nullptr) {   // the host launches the step only where it is built
-            if constexpr (kStepBuilt<FP8, PP, DEPTH>)
-                hipLaunchKernelGGL((attn_mfma_kernel<D, FP8, PP, DEPTH, false, true>), dim3(grid), dim3(kAttnBlock),
+            if constexpr (kStepBuilt<KV, PP, DEPTH>)
+                hipLaunchKernelGGL((attn_mfma_kernel<D, KV, PP, DEPTH, false, true>), dim3(grid), dim3(kAttnBlock),
                                    0, s, a);
             return;
         }
-        if constexpr (kTraced<D, FP8, PP, DEPTH>) {
+        if constexpr (kTraced<D, KV, PP, DEPTH>) {
             if (a.wave_times) {
-                hipLaunchKernelGGL((attn_mfma_kernel<D, FP8, PP, DEPTH, true, false>), dim3(grid), dim3(kAttnBlock),
+                hipLaunchKernelGGL((attn_mfma_kernel<D, KV, PP, DEPTH, true, false>), dim3(grid), dim3(kAttnBlock),
                                    0, s, a);
                 return;
             }
         }
-        hipLaunchKernelGGL((attn_mfma_kernel<D, FP8, PP, DEPTH, false, false>), dim3(grid), dim3(kAttnBlock), 0, s,
+        hipLaunchKernelGGL((attn_mfma_kernel<D, KV, PP, DEPTH, false, false>), dim3(grid), dim3(kAttnBlock), 0, s,
                            a);
     }
     static int occupancy() {
         int nb = 0;
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, attn_mfma_kernel<D, FP8, PP, DEPTH, false, false>,
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, attn_mfma_kernel<D, KV, PP, DEPTH, false, false>,
                                                          kAttnBlock, 0) != hipSuccess ||
             nb < 1)
             nb = 1;
@@ -1538,51 +1775,61 @@ struct Variant {
     }
 };
 
-// Dispatch on (head_dim, fp8, pages per step, depth): 1 or 2 pages for bf16
-// pools, 1, 2 or 4 for fp8 pools; depth 1 or 2.
-template <int D, bool FP8, int PP>
+// Dispatch on (head_dim, pool type, pages per step, depth): 1 or 2 pages for
+// bf16 pools, 1, 2 or 4 for fp8 pools, 4 for 4-bit pools; depth 1 or 2.
+template <int D, int KV, int PP>
 static int dispatch_depth(int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
     if (depth == 2) {
-        if (occ) return Variant<D, FP8, PP, 2>::occupancy();
-        Variant<D, FP8, PP, 2>::launch(*a, grid, s);
+        if (occ) return Variant<D, KV, PP, 2>::occupancy();
+        Variant<D, KV, PP, 2>::launch(*a, grid, s);
     } else {
-        if (occ) return Variant<D, FP8, PP, 1>::occupancy();
-        Variant<D, FP8, PP, 1>::launch(*a, grid, s);
+        if (occ) return Variant<D, KV, PP, 1>::occupancy();
+        Variant<D, KV, PP, 1>::launch(*a, grid, s);
     }
     return 0;
 }
 
-template <int D, bool FP8>
+template <int D, int KV>
 static int dispatch_pp(int pp, int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
-    if constexpr (FP8) {
-        if (pp == 4) return dispatch_depth<D, FP8, 4>(depth, occ, a, grid, s);
+    if constexpr (KV == kKvFp4) {
+        return dispatch_depth<D, KV, 4>(depth, occ, a, grid, s);
+    } else {
+        if constexpr (KV == kKvFp8) {
+            if (pp == 4) return dispatch_depth<D, KV, 4>(depth, occ, a, grid, s);
+        }
+        if (pp == 2) return dispatch_depth<D, KV, 2>(depth, occ, a, grid, s);
+        return dispatch_depth<D, KV, 1>(depth, occ, a, grid, s);
     }
-    if (pp == 2) return dispatch_depth<D, FP8, 2>(depth, occ, a, grid, s);
-    return dispatch_depth<D, FP8, 1>(depth, occ, a, grid, s);
 }
 
-static int dispatch(int D, bool fp8, int pp, int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
-    if (D == 128) return fp8 ? dispatch_pp<128, true>(pp, depth, occ, a, grid, s)
-                             : dispatch_pp<128, false>(pp, depth, occ, a, grid, s);
-    return fp8 ? dispatch_pp<64, true>(pp, depth, occ, a, grid, s) : dispatch_pp<64, false>(pp, depth, occ, a, grid, s);
+template <int D>
+static int dispatch_kv(int kv, int pp, int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
+    if (kv == kKvFp4) return dispatch_pp<D, kKvFp4>(pp, depth, occ, a, grid, s);
+    return kv == kKvFp8 ? dispatch_pp<D, kKvFp8>(pp, depth, occ, a, grid, s)
+                        : dispatch_pp<D, kKvBf16>(pp, depth, occ, a, grid, s);
 }
 
-void launch_attention(const AttnArgs& a, int pages_per_step, int depth, bool fp8, int grid, hipStream_t s) {
+static int dispatch(int D, int kv, int pp, int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
+    return D == 128 ? dispatch_kv<128>(kv, pp, depth, occ, a, grid, s) : dispatch_kv<64>(kv, pp, depth, occ, a, grid, s);
+}
+
+void launch_attention(const AttnArgs& a, int pages_per_step, int depth, int kv, int grid, hipStream_t s) {
     if (a.B == 0 || a.H_q == 0) return;
-    dispatch(a.D, fp8, pages_per_step, depth, false, &a, grid, s);
+    dispatch(a.D, kv, pages_per_step, depth, false, &a, grid, s);
 }
 
-bool attention_traced(int pages_per_step, int depth, bool fp8, int D) {
-    if (D != 128) return false;
-    return fp8 ? (pages_per_step == 4 && depth == 1) : (pages_per_step <= 2 && depth == 2);
+bool attention_traced(int pages_per_step, int depth, int kv, int D) {
+    if (D != 128 || kv == kKvFp4) return false;
+    return kv == kKvFp8 ? (pages_per_step == 4 && depth == 1) : (pages_per_step <= 2 && depth == 2);
 }
 
-bool attention_step_built(int pages_per_step, int depth, bool fp8) {
-    return fp8 ? (pages_per_step == 4 && depth == 1) : (pages_per_step <= 2 && depth == 2);
+bool attention_step_built(int pages_per_step, int depth, int kv) {
+    if (kv == kKvFp4) return false;
+    return kv == kKvFp8 ? (pages_per_step == 4 && depth == 1) : (pages_per_step <= 2 && depth == 2);
 }
 
-int attention_blocks_per_cu(int pages_per_step, int depth, bool fp8, int D) {
-    return dispatch(D, fp8, pages_per_step, depth, true, nullptr, 0, nullptr);
+int attention_blocks_per_cu(int pages_per_step, int depth, int kv, int D) {
+    return dispatch(D, kv, pages_per_step, depth, true, nullptr, 0, nullptr);
 }
 
 // The merge that deals each cut's pieces over a workgroup is taken where the

@@ -16,8 +16,9 @@
 namespace {
 
 PyObject *g_tensor, *g_parameter;             // the exact types taken
-PyObject* g_dtype[5];                         // torch dtypes, and their codes
-int32_t g_code[5];
+constexpr int kDtypes = 6;
+PyObject* g_dtype[kDtypes];                   // torch dtypes, and their codes
+int32_t g_code[kDtypes];
 PyObject *g_raw_stream, *g_device;            // current stream of a device, current device
 PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_is_contiguous;
 int g_float32 = -1;                           // index of float32 in g_dtype
@@ -49,7 +50,7 @@ bool device_tensor(PyObject* t) {
 
 int dtype_index(PyObject* t) {
     Ref r(PyObject_GetAttr(t, s_dtype));
-    for (int i = 0; i < 5; ++i)
+    for (int i = 0; i < kDtypes; ++i)
         if (r.p == g_dtype[i]) return i;
     return -1;
 }
@@ -93,10 +94,12 @@ bool fill(PyObject* t, PyObject* scale, bellman_tensor_t* d) {
 }
 
 // The calls' forms: tensors before and after the softmax scale, the position
-// of k_pages (v_pages follows), and whether the options come before the stream.
+// of k_pages (v_pages follows; -1: none), and whether the options come before
+// the stream; the tensors that may be None (bit i: tensor i).
 struct Form {
     int before, after, pages;
     bool opts;
+    unsigned optional = 0;
 };
 const Form kForms[] = {
     {6, 0, 2, false},   // 0 kv_append
@@ -105,18 +108,22 @@ const Form kForms[] = {
     {7, 1, 3, true},    // 3 decode_step
     {7, 0, 2, false},   // 4 kv_write
     {6, 1, 1, false},   // 5 prefill_attention
+    {7, 0, 0, false},   // 6 kv_read
+    {8, 0, -1, true, 0xc},   // 7 qk_norm_rope
 };
 
 typedef bellman_tensor_t T;
 
-int invoke(void* fn, int form, T* d, float scale, void* opts, void* stream) {
+// p: a null descriptor where a tensor is None
+int invoke(void* fn, int form, T* const* p, float scale, void* opts, void* stream) {
     switch (form) {
-        case 0: return ((int (*)(T*, T*, T*, T*, T*, T*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, d + 5, stream);
-        case 1: return ((int (*)(T*, T*, T*, T*, T*, float, T*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, scale, d + 5, stream);
-        case 2: return ((int (*)(T*, T*, T*, T*, T*, float, T*, void*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, scale, d + 5, opts, stream);
-        case 3: return ((int (*)(T*, T*, T*, T*, T*, T*, T*, float, T*, void*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, d + 5, d + 6, scale, d + 7, opts, stream);
-        case 4: return ((int (*)(T*, T*, T*, T*, T*, T*, T*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, d + 5, d + 6, stream);
-        default: return ((int (*)(T*, T*, T*, T*, T*, T*, float, T*, void*))fn)(d, d + 1, d + 2, d + 3, d + 4, d + 5, scale, d + 6, stream);
+        case 0: return ((int (*)(T*, T*, T*, T*, T*, T*, void*))fn)(p[0], p[1], p[2], p[3], p[4], p[5], stream);
+        case 1: return ((int (*)(T*, T*, T*, T*, T*, float, T*, void*))fn)(p[0], p[1], p[2], p[3], p[4], scale, p[5], stream);
+        case 2: return ((int (*)(T*, T*, T*, T*, T*, float, T*, void*, void*))fn)(p[0], p[1], p[2], p[3], p[4], scale, p[5], opts, stream);
+        case 3: return ((int (*)(T*, T*, T*, T*, T*, T*, T*, float, T*, void*, void*))fn)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], scale, p[7], opts, stream);
+        case 5: return ((int (*)(T*, T*, T*, T*, T*, T*, float, T*, void*))fn)(p[0], p[1], p[2], p[3], p[4], p[5], scale, p[6], stream);
+        case 7: return ((int (*)(T*, T*, T*, T*, T*, T*, T*, T*, void*, void*))fn)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], opts, stream);
+        default: return ((int (*)(T*, T*, T*, T*, T*, T*, T*, void*))fn)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], stream);   // 4, 6
     }
 }
 
@@ -139,8 +146,14 @@ PyObject* call(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const Form& f = kForms[form];
     T d[8];
+    T* p[8];
     for (int i = 0; i < (int)(n - kFixed); ++i) {
-        PyObject* s = i == f.pages ? a[5] : i == f.pages + 1 ? a[6] : Py_None;
+        p[i] = &d[i];
+        if (a[kFixed + i] == Py_None && (f.optional >> i & 1)) {
+            p[i] = nullptr;
+            continue;
+        }
+        PyObject* s = f.pages < 0 ? Py_None : i == f.pages ? a[5] : i == f.pages + 1 ? a[6] : Py_None;
         if (!fill(a[kFixed + i], s, &d[i])) {
             PyErr_Clear();
             Py_RETURN_NONE;
@@ -164,20 +177,20 @@ PyObject* call(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (PyErr_Occurred()) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = invoke(fn, (int)form, d, (float)scale, opts, stream);
+    rc = invoke(fn, (int)form, p, (float)scale, opts, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
 
-// setup(Tensor, Parameter, ((dtype, code), ...5), float32, raw_stream, device)
+// setup(Tensor, Parameter, ((dtype, code), ...6), float32, raw_stream, device)
 PyObject* setup(PyObject*, PyObject* args) {
     PyObject *tensor, *parameter, *dtypes, *f32, *raw, *dev;
     if (!PyArg_ParseTuple(args, "OOO!OOO", &tensor, &parameter, &PyTuple_Type, &dtypes, &f32, &raw, &dev)) return nullptr;
-    if (PyTuple_GET_SIZE(dtypes) != 5) {
-        PyErr_SetString(PyExc_ValueError, "setup: five element types");
+    if (PyTuple_GET_SIZE(dtypes) != kDtypes) {
+        PyErr_SetString(PyExc_ValueError, "setup: six element types");
         return nullptr;
     }
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < kDtypes; ++i) {
         PyObject* dt;
         int code;
         if (!PyArg_ParseTuple(PyTuple_GET_ITEM(dtypes, i), "Oi", &dt, &code)) return nullptr;

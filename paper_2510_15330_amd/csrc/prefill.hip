@@ -67,16 +67,23 @@ __device__ __forceinline__ int block_scan(int v, int* part) {
     return part[tid];
 }
 
-// Pages a request's new positions touch (token rows s0 .. s1 - 1 after L
-// cached ones), or -1 for a malformed request (negative or reversed range,
-// rows past T, negative length).
+// Pages a request's rows touch (token rows s0 .. s1 - 1: after L cached ones
+// for a write, the last of L for a read), or -1 for a malformed request
+// (negative or reversed range, rows past T, negative length; a read of more
+// rows than it has, or of a length past the table).
+template <bool READ>
 __device__ __forceinline__ int pages_touched(const WriteArgs& a, int s0, int s1, int L) {
     if (s0 < 0 || s1 < s0 || s1 > a.T || L < 0) return -1;
-    if (s1 == s0) return 0;
-    const int64_t last = (int64_t)L + (s1 - s0) - 1;
-    return (int)(last / kPage - L / kPage + 1);
+    const int64_t n = s1 - s0;
+    if (READ && (n > L || (int64_t)L > (int64_t)a.max_pages * kPage)) return -1;
+    if (n == 0) return 0;
+    const int64_t first = READ ? L - n : L;
+    return (int)((first + n - 1) / kPage - first / kPage + 1);
 }
+template <bool READ>
+constexpr int kErrPlan = READ ? kErrLength : kErrAppendSlot;
 
+template <bool READ>
 __global__ void __launch_bounds__(kPlanThreads) write_plan_kernel(WriteArgs a, int32_t* page_start) {
     __shared__ int part[kPlanThreads];
     __shared__ int malformed;
@@ -90,18 +97,18 @@ __global__ void __launch_bounds__(kPlanThreads) write_plan_kernel(WriteArgs a, i
         const int b = b0 + k;
         if (b >= a.B) break;
         if (a.q_start[b + 1] < a.q_start[b]) atomicOr(&malformed, 1);
-        const int t = pages_touched(a, a.q_start[b], a.q_start[b + 1], a.seq_lens[b]);
+        const int t = pages_touched<READ>(a, a.q_start[b], a.q_start[b + 1], a.seq_lens[b]);
         if (t < 0) bad = 1;
         else sum += t;
     }
-    if (bad) atomicOr(a.err, kErrAppendSlot);
+    if (bad) atomicOr(a.err, kErrPlan<READ>);
     const int incl = block_scan(sum, part);
     if (malformed) {
         for (int k = 0; k < per; ++k)
             if (b0 + k < a.B) page_start[b0 + k] = 0;
         if (tid == 0) {
             page_start[a.B] = 0;
-            atomicOr(a.err, kErrAppendSlot);
+            atomicOr(a.err, kErrPlan<READ>);
         }
         return;
     }
@@ -110,20 +117,23 @@ __global__ void __launch_bounds__(kPlanThreads) write_plan_kernel(WriteArgs a, i
         const int b = b0 + k;
         if (b < a.B) {
             page_start[b] = run;
-            run += max(pages_touched(a, a.q_start[b], a.q_start[b + 1], a.seq_lens[b]), 0);
+            run += max(pages_touched<READ>(a, a.q_start[b], a.q_start[b + 1], a.seq_lens[b]), 0);
         }
     }
     if (tid == kPlanThreads - 1) {
         page_start[a.B] = incl;
-        if (a.q_start[a.B] < a.T) atomicOr(a.err, kErrAppendSlot);   // rows no request owns
+        if (a.q_start[a.B] < a.T) atomicOr(a.err, kErrPlan<READ>);   // rows no request owns
     }
 }
 
-template <int EB>
-__global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a, const int32_t* page_start) {
-    __shared__ __attribute__((aligned(16))) uint8_t vst[kPage * 128 * 2];   // the page's V rows, one head
-    const int item = blockIdx.x, tid = threadIdx.x;
+// One item of the plan: page pi of request b, whose n rows start at token row
+// s0 and position L; false past the last item.
+struct WriteItem {
     int b, s0, L, n, pi;
+};
+template <bool READ>
+__device__ __forceinline__ bool write_item(const WriteArgs& a, const int32_t* page_start, WriteItem& w) {
+    const int item = blockIdx.x, tid = threadIdx.x;
     if (a.B <= 64) {
         // the plan, as write_plan_kernel makes it
         const int lane = tid & 63;
@@ -132,34 +142,44 @@ __global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a, const int32_
             q0 = a.q_start[lane];
             q1 = a.q_start[lane + 1];
             Lb = a.seq_lens[lane];
-            pages = pages_touched(a, q0, q1, Lb);
+            pages = pages_touched<READ>(a, q0, q1, Lb);
         }
         const int last = __builtin_amdgcn_readlane(q1, a.B - 1);
         const bool malformed = __builtin_amdgcn_readlane(q0, 0) < 0 || last > a.T || __ballot(q1 < q0) != 0;
         if (item == 0 && blockIdx.y == 0 && tid < 64 && (malformed || last < a.T || __ballot(pages < 0) != 0) && lane == 0)
-            atomicOr(a.err, kErrAppendSlot);
-        if (malformed) return;
+            atomicOr(a.err, kErrPlan<READ>);
+        if (malformed) return false;
         const int end = lane_scan(max(pages, 0));
-        if (item >= __builtin_amdgcn_readlane(end, 63)) return;
-        b = __ffsll((unsigned long long)__ballot(item < end)) - 1;      // the first whose pages end past item
-        s0 = __builtin_amdgcn_readlane(q0, b);
-        L = __builtin_amdgcn_readlane(Lb, b);
-        n = __builtin_amdgcn_readlane(q1, b) - s0;
-        pi = L / kPage + (item - (__builtin_amdgcn_readlane(end, b) - __builtin_amdgcn_readlane(pages, b)));
+        if (item >= __builtin_amdgcn_readlane(end, 63)) return false;
+        w.b = __ffsll((unsigned long long)__ballot(item < end)) - 1;      // the first whose pages end past item
+        w.s0 = __builtin_amdgcn_readlane(q0, w.b);
+        w.n = __builtin_amdgcn_readlane(q1, w.b) - w.s0;
+        w.L = __builtin_amdgcn_readlane(Lb, w.b) - (READ ? w.n : 0);
+        w.pi = w.L / kPage + (item - (__builtin_amdgcn_readlane(end, w.b) - __builtin_amdgcn_readlane(pages, w.b)));
     } else {
-        if (item >= page_start[a.B]) return;
+        if (item >= page_start[a.B]) return false;
         int lo = 0, hi = a.B - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (page_start[mid] <= item) lo = mid;
             else hi = mid - 1;
         }
-        b = lo;
-        s0 = a.q_start[b];
-        L = a.seq_lens[b];
-        n = a.q_start[b + 1] - s0;
-        pi = L / kPage + (item - page_start[b]);
+        w.b = lo;
+        w.s0 = a.q_start[lo];
+        w.n = a.q_start[lo + 1] - w.s0;
+        w.L = a.seq_lens[lo] - (READ ? w.n : 0);
+        w.pi = w.L / kPage + (item - page_start[lo]);
     }
+    return true;
+}
+
+template <int EB>
+__global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a, const int32_t* page_start) {
+    __shared__ __attribute__((aligned(16))) uint8_t vst[kPage * 128 * 2];   // the page's V rows, one head
+    const int tid = threadIdx.x;
+    WriteItem it;
+    if (!write_item<false>(a, page_start, it)) return;
+    const int b = it.b, s0 = it.s0, L = it.L, n = it.n, pi = it.pi;
     const int64_t first = (int64_t)kPage * pi;              // position of slot 0
     const int slot_lo = (int)(max((int64_t)L, first) - first);
     const int slot_hi = (int)(min((int64_t)L + n, first + kPage) - first);
@@ -224,6 +244,392 @@ __global__ void lens_kernel(WriteArgs a) {
         return;
     }
     a.seq_lens[b] = L + n;
+}
+
+// ------------------------------------------------------ 4-bit page write --
+// A wave takes a page of one head at a time.  Lane (blk, tok) quantises 32
+// dims of a token (bellman.h has the rule; the scaling is by powers of two, so
+// the bytes are determined) and so has K's 16 bytes and scale as they lie in
+// the tile.  V lies by 4-slot groups: the lanes' code words go through LDS,
+// and lane (q, n) gathers dims 16 t + n of slots 4q..4q+3 into its own 16
+// bytes.  Bytes of V that hold slots outside the request's new rows keep those
+// slots' codes.  Bound by memory: rows read once, the tile written once.
+constexpr uint32_t kNan4 = 255u;
+
+// The scale byte of a block whose largest magnitude has the bf16 bits m.
+__device__ __forceinline__ uint32_t scale4(uint32_t m) {
+    // one more than the exponent where the fraction is above 1.75
+    return m >= 0x7f80u ? kNan4 : (uint32_t)min(max((int)((m + 0x1fu) >> 7) - 2, 0), 252);
+}
+
+// 16 words of bf16 pairs -> 32 codes in 4 words, and the scale byte.
+__device__ __forceinline__ uint32_t quantize4(const uint32_t (&in)[16], u32x4& codes) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, in[i] & 0x7fff7fffu));
+    const uint32_t s = scale4(max((uint32_t)m.x, (uint32_t)m.y));
+    const float inv = __uint_as_float((254u - min(s, 252u)) << 23);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w = 0;
+        const float lo[4] = {__uint_as_float(in[4 * i] << 16) * inv, __uint_as_float(in[4 * i + 1] << 16) * inv,
+                             __uint_as_float(in[4 * i + 2] << 16) * inv, __uint_as_float(in[4 * i + 3] << 16) * inv};
+        const float hi[4] = {__uint_as_float(in[4 * i] & 0xffff0000u) * inv,
+                             __uint_as_float(in[4 * i + 1] & 0xffff0000u) * inv,
+                             __uint_as_float(in[4 * i + 2] & 0xffff0000u) * inv,
+                             __uint_as_float(in[4 * i + 3] & 0xffff0000u) * inv};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[0], hi[0], 1.0f, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[1], hi[1], 1.0f, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[2], hi[2], 1.0f, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[3], hi[3], 1.0f, 3);
+        codes[i] = s == kNan4 ? 0u : w;
+    }
+    return s;
+}
+
+__device__ __forceinline__ void wave_lds_fence() {   // one wave's LDS writes before its other lanes' reads
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv4_write_kernel(WriteArgs a, const int32_t* page_start) {
+    // [token][dim / 8 mod 2][dim / 16] code words, a row padded to spread the banks
+    constexpr int ROW = D / 8 + 4;
+    __shared__ __attribute__((aligned(16))) uint32_t vst[4][kPage * ROW];
+    const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    WriteItem it;
+    if (!write_item<false>(a, page_start, it)) return;
+    const int64_t first = (int64_t)kPage * it.pi;           // position of slot 0
+    const int slot_lo = (int)(max((int64_t)it.L, first) - first);
+    const int slot_hi = (int)(min((int64_t)it.L + it.n, first + kPage) - first);
+    int pg = -1;
+    if (it.pi < a.max_pages) pg = a.block_table[(int64_t)it.b * a.bt_stride + it.pi];
+    if (pg < 0 || pg >= a.num_pages) {
+        if (blockIdx.y == 0 && threadIdx.x == 0) atomicOr(a.err, kErrAppendSlot);
+        return;
+    }
+    const int64_t row0 = it.s0 + (first - it.L);            // token row of slot 0
+    constexpr int TB = kTile4Rows * D / 2;
+    const int blk = D == 128 ? qg : qg & 1;
+    const bool live = n >= slot_lo && n < slot_hi;
+    for (int g = blockIdx.y * 4 + w; g < a.H_kv; g += 4 * gridDim.y) {
+        char* kp = (char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
+        char* vp = (char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * TB;
+        const uint16_t* kn = (const uint16_t*)a.k_new + (row0 + n) * a.k_st + (int64_t)g * a.k_sh + 32 * blk;
+        const uint16_t* vn = (const uint16_t*)a.v_new + (row0 + n) * a.v_st + (int64_t)g * a.v_sh + 32 * blk;
+        constexpr int NP = D == 128 ? 2 : 1;    // head_dim 64: lanes 0-31 take K, 32-63 V
+        uint32_t in[NP][16];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const uint16_t* src = (D == 128 ? p == 1 : lane >= 32) ? vn : kn;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x4 x = live ? *(const u32x4*)(src + 8 * i) : u32x4{0u, 0u, 0u, 0u};
+                in[p][4 * i] = x.x;
+                in[p][4 * i + 1] = x.y;
+                in[p][4 * i + 2] = x.z;
+                in[p][4 * i + 3] = x.w;
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const bool isv = D == 128 ? p == 1 : lane >= 32;
+            u32x4 c;
+            const uint32_t s = quantize4(in[p], c);
+            if (!isv) {
+                if (live) {
+                    *(u32x4*)(kp + blk * 256 + n * 16) = c;
+                    *(uint8_t*)(kp + 8 * D + blk * 16 + n) = (uint8_t)s;
+                }
+            } else {
+                if (live) *(uint8_t*)(vp + 8 * D + (n >> 2) * (D / 8) + 4 * blk + (n & 3)) = (uint8_t)s;
+                uint32_t* row = &vst[w][n * ROW];
+                *(u32x2*)(row + 2 * blk) = u32x2{c.x, c.z};
+                *(u32x2*)(row + D / 16 + 2 * blk) = u32x2{c.y, c.w};
+            }
+        }
+        wave_lds_fence();
+        // lane (q, n): dims 16 t + n of slots 4q .. 4q + 3, nibble r of halfword t
+        const int q = qg, sh = 4 * (n & 7);
+        uint32_t o[D / 32];
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) o[b] = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t* row = &vst[w][(4 * q + r) * ROW + (n >> 3) * (D / 16)];
+#pragma unroll
+            for (int t4 = 0; t4 < D / 64; ++t4) {
+                const u32x4 x = *(const u32x4*)(row + 4 * t4);
+                o[2 * t4] |= ((x.x >> sh) & 15u) << (4 * r) | ((x.y >> sh) & 15u) << (16 + 4 * r);
+                o[2 * t4 + 1] |= ((x.z >> sh) & 15u) << (4 * r) | ((x.w >> sh) & 15u) << (16 + 4 * r);
+            }
+        }
+        wave_lds_fence();           // the next head's words come after these reads
+        const int k0 = max(slot_lo - 4 * q, 0), k1 = min(slot_hi - 4 * q, 4);   // live slots of the quad
+        if (k0 < k1) {
+            using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
+            VT* dst = (VT*)(vp + lane * (D / 8));
+            VT x;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b) x[b] = o[b];
+            if (k1 - k0 < 4) {
+                const uint32_t m = ((1u << (4 * k1)) - (1u << (4 * k0))) * 0x10001u;
+                const VT old = *dst;
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) x[b] = (old[b] & ~m) | (x[b] & m);
+            }
+            *dst = x;
+        }
+    }
+}
+
+// One request's token into 4-bit pages: wave pairs take four heads at a time,
+// one wave their K rows, the other their V rows, 16 lanes a row.  K: 8 dims a
+// lane (D = 128; 4 at 64), a block's maximum over 4 (8) lanes.  V: dims 16 t + n,
+// a block's maximum over the row's lanes, and the lane's 16 bytes of the slot's
+// group read, one nibble of each halfword set, and written back.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {   // over the 16 lanes of a row
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));   // row_ror 8, 4, 2, 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));
+    return v;
+}
+
+// One bf16 value's code under the scale byte s.
+__device__ __forceinline__ uint32_t code4(uint32_t bits, uint32_t s) {
+    const float y = __uint_as_float(bits << 16) * __uint_as_float((254u - min(s, 252u)) << 23);
+    return s == kNan4 ? 0u : (uint32_t)__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y, 0.f, 1.0f, 0) & 15u;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv4_append_kernel(AppendArgs a) {
+    constexpr int TB = kTile4Rows * D / 2;
+    constexpr int E = D / 16;             // dims a lane
+    const int b = blockIdx.x, lane = threadIdx.x & 63, n = lane & 15;
+    const int w = threadIdx.x >> 6;
+    const int L = a.seq_lens[b];
+    const int pi = L >> 4;
+    const bool in_table = L >= 0 && pi < a.max_pages;
+    const int pg = in_table ? a.block_table[(int64_t)b * a.bt_stride + pi] : -1;
+    const bool ok = pg >= 0 && (int64_t)pg < a.num_pages;
+    if (!ok && threadIdx.x == 0) atomicOr(a.err, kErrAppendSlot);
+    if (!ok) return;
+    const int slot = L & (kPage - 1), q = slot >> 2, r = slot & 3;
+    for (int g = (w >> 1) * 4 + (lane >> 4); g < a.H_kv; g += 8) {
+        if ((w & 1) == 0) {
+            const uint16_t* kn = (const uint16_t*)a.k_new + (int64_t)b * a.new_sb + (int64_t)g * a.new_sh + E * n;
+            char* kp = (char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
+            uint32_t in[E / 2];
+#pragma unroll
+            for (int i = 0; i < E / 2; i += 2) {
+                const u32x2 x = *(const u32x2*)(kn + 2 * i);
+                in[i] = x.x;
+                in[i + 1] = x.y;
+            }
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) m = max(m, max(in[i] & 0x7fffu, (in[i] >> 16) & 0x7fffu));
+            // over the lanes of a block: quad_perm 1 0 3 2, then 2 3 0 1 (and at 8 lanes row_half_mirror)
+            m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));
+            m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true));
+            if constexpr (D == 64) m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, true));
+            const uint32_t s = scale4(m);
+            uint32_t c = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) c |= code4((in[i / 2] >> (16 * (i & 1))) & 0xffffu, s) << (4 * i);
+            const int blk = E * n / 32, at = (E * n % 32) / 2;     // the lane's bytes of the slot's 16
+            char* dst = kp + blk * 256 + slot * 16 + at;
+            if constexpr (D == 128) *(uint32_t*)dst = c;
+            else *(uint16_t*)dst = (uint16_t)c;
+            if (at == 0) *(uint8_t*)(kp + 8 * D + blk * 16 + slot) = (uint8_t)s;
+        } else {
+            const uint16_t* vn = (const uint16_t*)a.v_new + (int64_t)b * a.vnew_sb + (int64_t)g * a.vnew_sh + n;
+            char* vp = (char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * TB;
+            using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
+            VT* dst = (VT*)(vp + (q * 16 + n) * (D / 8));
+            VT x = *dst;
+            uint32_t in[E];
+#pragma unroll
+            for (int t = 0; t < E; ++t) in[t] = vn[16 * t];
+#pragma unroll
+            for (int blk = 0; blk < D / 32; ++blk) {
+                const uint32_t s = scale4(row_max(max(in[2 * blk] & 0x7fffu, in[2 * blk + 1] & 0x7fffu)));
+                const uint32_t c = code4(in[2 * blk], s) << (4 * r) | code4(in[2 * blk + 1], s) << (16 + 4 * r);
+                x[blk] = (x[blk] & ~(0x000f000fu << (4 * r))) | c;
+                if (n == blk) *(uint8_t*)(vp + 8 * D + q * (D / 8) + 4 * blk + r) = (uint8_t)s;
+            }
+            *dst = x;
+        }
+    }
+    __syncthreads();  // every thread has read seq_lens[b]
+    if (threadIdx.x == 0) a.seq_lens[b] = L + 1;
+}
+
+// ---------------------------------------------------------------- read back --
+// The rows that the pages hold, as bf16: the plan of a write, from the other
+// side.  A row whose page lies outside the pool is NaN (flagged).
+
+// 2^(s - 127) of a scale byte: a denormal at 0, NaN at 255
+__device__ __forceinline__ float scale_of4(uint32_t s) {
+    return __uint_as_float(s == 0u ? 0x00400000u : s == kNan4 ? 0x7fc00000u : s << 23);
+}
+// byte i of w (two codes) times sc, exactly, as two bf16 (beyond bf16's range: inf)
+__device__ __forceinline__ uint32_t pair4_bf16(f32x2 v) {
+    return __builtin_amdgcn_perm(__float_as_uint(v.y), __float_as_uint(v.x), 0x07060302u);
+}
+template <int BYTE>
+__device__ __forceinline__ f32x2 pair4(uint32_t w, float sc) {
+    const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, BYTE);
+    return f32x2{v.x * sc, v.y * sc};
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv4_read_kernel(WriteArgs a, const int32_t* page_start) {
+    constexpr int ROW = D + 8;               // a V row of bf16 in LDS
+    __shared__ __attribute__((aligned(16))) uint16_t vst[4][kPage * ROW];
+    const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    WriteItem it;
+    if (!write_item<true>(a, page_start, it)) return;
+    const int64_t first = (int64_t)kPage * it.pi;
+    const int slot_lo = (int)(max((int64_t)it.L, first) - first);
+    const int slot_hi = (int)(min((int64_t)it.L + it.n, first + kPage) - first);
+    int pg = a.block_table[(int64_t)it.b * a.bt_stride + it.pi];
+    const bool ok = pg >= 0 && pg < a.num_pages;
+    if (!ok) {
+        pg = 0;
+        if (blockIdx.y == 0 && threadIdx.x == 0) atomicOr(a.err, kErrPage);
+    }
+    const int64_t row0 = it.s0 + (first - it.L);
+    constexpr int TB = kTile4Rows * D / 2;
+    const int blk = D == 128 ? qg : qg & 1;
+    const bool live = n >= slot_lo && n < slot_hi && (D == 128 || lane < 32);
+    const u32x4 nan4 = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    for (int g = blockIdx.y * 4 + w; g < a.H_kv; g += 4 * gridDim.y) {
+        const char* kp = (const char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
+        const char* vp = (const char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * TB;
+        const u32x4 kc = *(const u32x4*)(kp + blk * 256 + n * 16);
+        const float ks = scale_of4(*(const uint8_t*)(kp + 8 * D + blk * 16 + n));
+        using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
+        const VT vc = *(const VT*)(vp + lane * (D / 8));
+        const VT vs = *(const VT*)(vp + 8 * D + qg * (D / 8));
+        // lane (q, n): slots 4q .. 4q + 3 of dims 16 t + n
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            float sc[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[r] = scale_of4((vs[b] >> (8 * r)) & 255u);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const f32x2 v01 = t ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[b], 1.0f, 2)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[b], 1.0f, 0);
+                const f32x2 v23 = t ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[b], 1.0f, 3)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[b], 1.0f, 1);
+                const float v[4] = {v01.x * sc[0], v01.y * sc[1], v23.x * sc[2], v23.y * sc[3]};
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    vst[w][(4 * qg + r) * ROW + 32 * b + 16 * t + n] = (uint16_t)(__float_as_uint(v[r]) >> 16);
+            }
+        }
+        wave_lds_fence();
+        if (live) {
+            uint16_t* ko = (uint16_t*)a.k_new + (row0 + n) * a.k_st + (int64_t)g * a.k_sh + 32 * blk;
+            uint16_t* vo = (uint16_t*)a.v_new + (row0 + n) * a.v_st + (int64_t)g * a.v_sh + 32 * blk;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x4 x = {pair4_bf16(pair4<0>(kc[i], ks)), pair4_bf16(pair4<1>(kc[i], ks)),
+                                 pair4_bf16(pair4<2>(kc[i], ks)), pair4_bf16(pair4<3>(kc[i], ks))};
+                *(u32x4*)(ko + 8 * i) = ok ? x : nan4;
+                const u32x4 y = *(const u32x4*)&vst[w][n * ROW + 32 * blk + 8 * i];
+                *(u32x4*)(vo + 8 * i) = ok ? y : nan4;
+            }
+        }
+        wave_lds_fence();
+    }
+}
+
+// bf16 pools (copies) and fp8 pools (code times the (request, head)'s scale,
+// rounded to nearest even).
+template <int EB>
+__global__ void __launch_bounds__(256) kv_read_kernel(WriteArgs a, const int32_t* page_start) {
+    __shared__ __attribute__((aligned(16))) uint16_t vst[kPage * (128 + 8)];
+    const int tid = threadIdx.x;
+    WriteItem it;
+    if (!write_item<true>(a, page_start, it)) return;
+    const int64_t first = (int64_t)kPage * it.pi;
+    const int slot_lo = (int)(max((int64_t)it.L, first) - first);
+    const int slot_hi = (int)(min((int64_t)it.L + it.n, first + kPage) - first);
+    int pg = a.block_table[(int64_t)it.b * a.bt_stride + it.pi];
+    const bool ok = pg >= 0 && pg < a.num_pages;
+    if (!ok) {
+        pg = 0;
+        if (blockIdx.y == 0 && tid == 0) atomicOr(a.err, kErrPage);
+    }
+    const int64_t row0 = it.s0 + (first - it.L);
+    constexpr int x = 16 / EB;
+    const int row = a.D + 8;
+    const u32x4 nan4 = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    // four codes times sc -> four bf16
+    auto widen = [](uint32_t w, float sc) {
+        const f32x2 v0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), v1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        const f32x2 y0 = {v0.x * sc, v0.y * sc}, y1 = {v1.x * sc, v1.y * sc};
+        return u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(y0, bf16x2)),
+                     __builtin_bit_cast(uint32_t, __builtin_convertvector(y1, bf16x2))};
+    };
+    for (int g = blockIdx.y; g < a.H_kv; g += gridDim.y) {
+        if (g != (int)blockIdx.y) __syncthreads();
+        const char* kp = (const char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * (int64_t)a.D * kPage * EB;
+        const char* vp = (const char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * (int64_t)a.D * kPage * EB;
+        float ks = 1.f, vs = 1.f;
+        if (EB == 1) {
+            ks = a.k_scale[(int64_t)it.b * a.H_kv + g];
+            vs = a.v_scale[(int64_t)it.b * a.H_kv + g];
+        }
+        for (int u = tid; u < a.D / x * kPage; u += 256) {
+            const int c = u / kPage, sl = u % kPage;
+            if (sl < slot_lo || sl >= slot_hi) continue;
+            const u32x4 k = *(const u32x4*)(kp + (int64_t)u * 16);
+            uint16_t* dst = (uint16_t*)a.k_new + (row0 + sl) * a.k_st + (int64_t)g * a.k_sh + (int64_t)c * x;
+            if (EB == 2) {
+                *(u32x4*)dst = ok ? k : nan4;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x2 l = widen(k[2 * i], ks), h = widen(k[2 * i + 1], ks);
+                    *(u32x4*)(dst + 8 * i) = ok ? u32x4{l.x, l.y, h.x, h.y} : nan4;
+                }
+            }
+        }
+        // V page rows: unit (d, h) holds slots h x .. h x + x - 1 of dim d
+        for (int u = tid; u < a.D * EB; u += 256) {
+            const int d = u / EB, h = u % EB;
+            const u32x4 v = *(const u32x4*)(vp + (int64_t)u * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x2 e = EB == 2 ? u32x2{v[i], 0u} : widen(v[i], vs);
+                const int sl = h * x + i * (x / 4);
+                vst[sl * row + d] = (uint16_t)e.x;
+                vst[(sl + 1) * row + d] = (uint16_t)(e.x >> 16);
+                if (EB == 1) {
+                    vst[(sl + 2) * row + d] = (uint16_t)e.y;
+                    vst[(sl + 3) * row + d] = (uint16_t)(e.y >> 16);
+                }
+            }
+        }
+        __syncthreads();
+        for (int u = tid; u < kPage * a.D / 8; u += 256) {
+            const int sl = u / (a.D / 8), k = u % (a.D / 8);
+            if (sl < slot_lo || sl >= slot_hi) continue;
+            uint16_t* dst = (uint16_t*)a.v_new + (row0 + sl) * a.v_st + (int64_t)g * a.v_sh + 8 * k;
+            *(u32x4*)dst = ok ? *(const u32x4*)&vst[sl * row + 8 * k] : nan4;
+        }
+    }
 }
 
 // --------------------------------------------------------------- planning --
@@ -499,6 +905,105 @@ __global__ void __launch_bounds__(256) vcopy_kernel(PrefillArgs a) {
     }
 }
 
+// 4-bit pools: the keys are copied too, widened exactly to bf16 in the bf16
+// pools' layout, and the values to fp16 at their step's scale as above.  Wave w
+// takes page w of the step: lane (blk, tok) 32 dims of a key, lane (q, n) dims
+// 16 t + n of slots 4q..4q+3.  A page outside the pool leaves NaN keys.
+template <int D>
+__global__ void __launch_bounds__(256) kv4copy_kernel(PrefillArgs a) {
+    constexpr int TB = kTile4Rows * D / 2;
+    using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
+    __shared__ float wmax[2][4];
+    const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int blk = D == 128 ? qg : qg & 1;
+    const bool self = a.B <= 64;
+    int s_end = 0, total, Lb = 0;
+    if (self) {
+        const WavePlan p(a, false, 0);
+        s_end = lane_scan(p.r.steps);
+        total = __builtin_amdgcn_readlane(s_end, 63);
+        s_end -= p.r.steps;         // first step of this lane's request
+        Lb = p.r.steps > 0 ? p.r.L : 0;
+    } else {
+        total = a.step_off[a.B];
+    }
+    int par = 0;
+    for (int64_t t = blockIdx.x; t < (int64_t)total * a.H_kv; t += gridDim.x, par ^= 1) {
+        const int p = (int)(t / a.H_kv), g = (int)(t % a.H_kv);
+        int b, j, L;
+        if (self) {
+            const uint64_t m = __ballot(Lb > 0 && s_end <= p);
+            b = 63 - __clzll((long long)m);
+            j = p - __builtin_amdgcn_readlane(s_end, b);
+            L = __builtin_amdgcn_readlane(Lb, b);
+        } else {
+            b = a.step_req[p];
+            j = p - a.step_off[b];
+            L = a.seq_lens[b];
+        }
+        const int pi = (kPrefillKeys / kPage) * j + w;
+        const int nv = max(min(L - kPage * pi, kPage), 0);        // live slots of this wave's page
+        const int pg = nv > 0 ? a.block_table[(int64_t)b * a.bt_stride + pi] : 0;
+        const bool ok = (unsigned)pg < (unsigned)a.num_pages;
+        if (!ok && lane == 0) atomicOr(a.err, kErrPage);
+        const int64_t tile = ((int64_t)(ok ? pg : 0) * a.H_kv + g) * TB;
+        const char* kp = (const char*)a.k_pages + tile;
+        const char* vp = (const char*)a.v_pages + tile;
+        const u32x4 kc = *(const u32x4*)(kp + blk * 256 + n * 16);
+        const uint32_t ksb = *(const uint8_t*)(kp + 8 * D + blk * 16 + n);
+        const VT vc = *(const VT*)(vp + lane * (D / 8));
+        const VT vs = *(const VT*)(vp + 8 * D + qg * (D / 8));
+        float v[D / 16][4];
+        float m = 0.f;
+#pragma unroll
+        for (int bb = 0; bb < D / 32; ++bb) {
+            float sc[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[r] = scale_of4((vs[bb] >> (8 * r)) & 255u);
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const f32x2 v01 = tt ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[bb], 1.0f, 2)
+                                     : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[bb], 1.0f, 0);
+                const f32x2 v23 = tt ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[bb], 1.0f, 3)
+                                     : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[bb], 1.0f, 1);
+                const float y[4] = {v01.x * sc[0], v01.y * sc[1], v23.x * sc[2], v23.y * sc[3]};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    v[2 * bb + tt][r] = 4 * qg + r < nv ? y[r] : 0.f;
+                    m = fmaxf(m, fabsf(v[2 * bb + tt][r]));
+                }
+            }
+        }
+        const int64_t page = (t * (kPrefillKeys / kPage) + w) * (int64_t)(D * kPage);
+        if (D == 128 || lane < 32) {
+            // NaN, or 0 past the length
+            const float ks = !ok ? __uint_as_float(0x7fc00000u) : n < nv ? scale_of4(ksb) : 0.f;
+            uint16_t* dst = a.kcopy + page + blk * (4 * kPage * 8) + n * 8;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(u32x4*)(dst + i * (kPage * 8)) =
+                    u32x4{pair4_bf16(pair4<0>(kc[i], ks)), pair4_bf16(pair4<1>(kc[i], ks)),
+                          pair4_bf16(pair4<2>(kc[i], ks)), pair4_bf16(pair4<3>(kc[i], ks))};
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        if (lane == 0) wmax[par][w] = m;
+        __syncthreads();            // two sets in turn: the next step's writes cannot pass this step's reads
+        m = fmaxf(fmaxf(wmax[par][0], wmax[par][1]), fmaxf(wmax[par][2], wmax[par][3]));
+        const int e = vcopy_exp(__float_as_uint(m));
+        if (threadIdx.x == 0) a.vexp[t] = e;
+        const float sc = e == kAnyExp ? 1.f : pow2f(e);
+        uint16_t* dst = a.vcopy + page + n * kPage + 4 * qg;
+#pragma unroll
+        for (int tt = 0; tt < D / 16; ++tt) {
+            const f32x2 lo = {v[tt][0] * sc, v[tt][1] * sc}, hi = {v[tt][2] * sc, v[tt][3] * sc};
+            *(u32x2*)(dst + tt * (16 * kPage)) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, f16x2)),
+                                                       __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, f16x2))};
+        }
+    }
+}
+
 // -------------------------------------------------------------- attention --
 // Workgroup = a unit of the plan: 128 query rows of one request and KV head
 // over a range of its keys; wave w owns rows 32w..32w+31.  Keys go by steps
@@ -564,7 +1069,9 @@ constexpr int kValuPerMfma = 7;
 // Pages sit PB + 128 bytes apart in LDS and odd pages hold K slot s at
 // s ^ 4, so every 8 (and 16) consecutive lanes of a read touch distinct
 // banks.
-template <int D, int NH, bool FP8>
+//
+// KC (4-bit pools): K tiles too come from a copy, laid out as bf16 pools are.
+template <int D, int NH, bool FP8, bool KC>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_attn_kernel(PrefillArgs a) {
     constexpr int KS = 32 * NH;         // keys per step
@@ -582,7 +1089,7 @@ prefill_attn_kernel(PrefillArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t kb1[KTW];
     __shared__ __attribute__((aligned(16))) uint16_t vb0[KTW];
     __shared__ __attribute__((aligned(16))) uint16_t vb1[KTW];
-    __shared__ int pages[kPageWindow];
+    __shared__ int pages[KC ? 1 : kPageWindow];
     __shared__ int vexps[FP8 ? 1 : WIN];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -694,14 +1201,14 @@ prefill_attn_kernel(PrefillArgs a) {
 #pragma unroll
         for (int k = 0; k < kPageWindow / 256; ++k) {
             const int e = 256 * k + tid;
-            if (e >= e0 && e < e1) pe[k] = bt[min(PPS * j + e, np - 1)];
+            if (!KC && e >= e0 && e < e1) pe[k] = bt[min(PPS * j + e, np - 1)];
         }
         const bool mine = !FP8 && PPS * tid >= e0 && PPS * tid < e1;
         if (mine) ve = a.vexp[(int64_t)(vstep0 + j + tid) * a.H_kv + g];
 #pragma unroll
         for (int k = 0; k < kPageWindow / 256; ++k) {
             const int e = 256 * k + tid;
-            if (e >= e0 && e < e1) pages[e] = pe[k];
+            if (!KC && e >= e0 && e < e1) pages[e] = pe[k];
         }
         if (mine) vexps[tid] = ve;
         __syncthreads();
@@ -718,8 +1225,10 @@ prefill_attn_kernel(PrefillArgs a) {
     // bf16 pools: the values come from the fp16 copy, whose steps of request b
     // are consecutive from vstep0
     const char* vbase16 = FP8 ? nullptr : (const char*)a.vcopy + ((int64_t)vstep0 * a.H_kv + g) * (PPS * PB);
+    const char* kbase16 = KC ? (const char*)a.kcopy + ((int64_t)vstep0 * a.H_kv + g) * (PPS * PB) : nullptr;
     int64_t off1[PPS], off2[PPS];      // page byte offsets of steps s + 1 and s + 2
     auto pages_of = [&](int j, int64_t (&off)[PPS]) {
+        if constexpr (KC) return;
         const int e = PPS * (j % WIN);
 #pragma unroll
         for (int q = 0; q < PPS; ++q) {
@@ -778,6 +1287,21 @@ prefill_attn_kernel(PrefillArgs a) {
             const int vg = v ^ (((v >> 3) ^ (v >> 4)) & 1);
             __builtin_amdgcn_global_load_lds(src + (256 * k + 64 * w - v + lane + vg) * 16, dst + 8 * (256 * k + 64 * w), 16,
                                              0, 0);
+        }
+    };
+    // the keys of step j: from the pool's pages, or from their copy
+    auto dma_k = [&](int j, const int64_t (&off)[PPS], uint16_t* dst) {
+        if constexpr (!KC) {
+            dma(kbase, off, dst, false);
+        } else {
+            const char* src = kbase16 + (int64_t)j * a.H_kv * (PPS * PB);
+#pragma unroll
+            for (int k = 0; k < PERH; ++k) {
+                const int v = ((256 * k + 64 * w) % UPP) + lane;
+                const int vg = v ^ (((v >> 3) & 1) << 2);
+                __builtin_amdgcn_global_load_lds(src + (256 * k + 64 * w - v + lane + vg) * 16,
+                                                 dst + 8 * (256 * k + 64 * w), 16, 0, 0);
+            }
         }
     };
     // fp8: V slots of keys >= L hold no token (NaN in a pool); P is 0 there,
@@ -876,7 +1400,7 @@ prefill_attn_kernel(PrefillArgs a) {
         refill(s_lo / WIN * WIN);
         pages_of(s_lo, off2);
         e1 = vexp_of(s_lo);
-        dma(kbase, off2, kb0, false);
+        dma_k(s_lo, off2, kb0);
         if constexpr (FP8) dma(vbase, off2, vb0, true);
         else dma_v16(s_lo, vb0);
         if (s_lo + 1 < s_hi) {
@@ -886,7 +1410,7 @@ prefill_attn_kernel(PrefillArgs a) {
             }
             pages_of(s_lo + 1, off1);
             e2 = vexp_of(s_lo + 1);
-            dma(kbase, off1, kb1, false);
+            dma_k(s_lo + 1, off1, kb1);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -917,7 +1441,7 @@ prefill_attn_kernel(PrefillArgs a) {
             if ((s + 2) % WIN == 0) refill(s + 2);
             pages_of(s + 2, off2);
             e3 = vexp_of(s + 2);
-            dma(kbase, off2, k_wr, false);
+            dma_k(s + 2, off2, k_wr);
         }
         // the weights' factor 2^-d of this step, as the exponent's offset, and
         // 2^d, which takes their sum back (d in [-7, 0], above 0 only past
@@ -1170,10 +1694,12 @@ __global__ void __launch_bounds__(256) prefill_merge_kernel(PrefillArgs a) {
 
 }  // namespace
 
+// An upper bound on the pages touched: ceil(n_b / 16) + 1 per request.
+static unsigned write_items(const WriteArgs& a) { return (unsigned)(a.T / kPage + 2 * a.B + 1); }
+
 void launch_kv_write(const WriteArgs& a, int32_t* page_start, hipStream_t s) {
-    if (a.B > 64) hipLaunchKernelGGL(write_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, page_start);
-    // an upper bound on the pages touched: ceil(n_b / 16) + 1 per request
-    const unsigned items = (unsigned)(a.T / kPage + 2 * a.B + 1);
+    if (a.B > 64) hipLaunchKernelGGL(write_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, a, page_start);
+    const unsigned items = write_items(a);
     // the heads of a page go over as many workgroups as it takes to have 4096,
     // so that the plan each makes is spread over the rest: 30k tokens of 8
     // heads 48.5 us with a workgroup a head, 42.6 us with three heads each
@@ -1181,14 +1707,47 @@ void launch_kv_write(const WriteArgs& a, int32_t* page_start, hipStream_t s) {
     // chats' 1.1k tokens 4.6 + 6.0 -> 6.0 us)
     const unsigned ny = std::min((unsigned)a.H_kv, 4096u / std::min(items, 4096u) + 1);
     const dim3 grid(items, ny);
-    if (a.elem_bytes == 2) hipLaunchKernelGGL(kv_write_kernel<2>, grid, dim3(256), 0, s, a, (const int32_t*)page_start);
-    else hipLaunchKernelGGL(kv_write_kernel<1>, grid, dim3(256), 0, s, a, (const int32_t*)page_start);
+    if (a.kv == kKvFp4) {
+        const dim3 g4(items, std::min((unsigned)(a.H_kv + 3) / 4, ny));   // a wave a head
+        if (a.D == 128) hipLaunchKernelGGL(kv4_write_kernel<128>, g4, dim3(256), 0, s, a, (const int32_t*)page_start);
+        else hipLaunchKernelGGL(kv4_write_kernel<64>, g4, dim3(256), 0, s, a, (const int32_t*)page_start);
+    } else if (a.elem_bytes == 2) {
+        hipLaunchKernelGGL(kv_write_kernel<2>, grid, dim3(256), 0, s, a, (const int32_t*)page_start);
+    } else {
+        hipLaunchKernelGGL(kv_write_kernel<1>, grid, dim3(256), 0, s, a, (const int32_t*)page_start);
+    }
     hipLaunchKernelGGL(lens_kernel, dim3((a.B + 255) / 256), dim3(256), 0, s, a);
+}
+
+void launch_kv4_append(const AppendArgs& a, hipStream_t s) {
+    if (a.D == 128) hipLaunchKernelGGL(kv4_append_kernel<128>, dim3(a.B), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(kv4_append_kernel<64>, dim3(a.B), dim3(256), 0, s, a);
+}
+
+void launch_kv_read(const WriteArgs& a, int32_t* page_start, hipStream_t s) {
+    if (a.B > 64) hipLaunchKernelGGL(write_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, a, page_start);
+    const unsigned items = write_items(a);
+    const unsigned ny = std::min((unsigned)a.H_kv, 4096u / std::min(items, 4096u) + 1);   // as for the write
+    const dim3 grid(items, ny), g4(items, std::min((unsigned)(a.H_kv + 3) / 4, ny));
+    const int32_t* ps = page_start;
+    if (a.kv == kKvFp4) {
+        if (a.D == 128) hipLaunchKernelGGL(kv4_read_kernel<128>, g4, dim3(256), 0, s, a, ps);
+        else hipLaunchKernelGGL(kv4_read_kernel<64>, g4, dim3(256), 0, s, a, ps);
+    } else if (a.elem_bytes == 2) {
+        hipLaunchKernelGGL(kv_read_kernel<2>, grid, dim3(256), 0, s, a, ps);
+    } else {
+        hipLaunchKernelGGL(kv_read_kernel<1>, grid, dim3(256), 0, s, a, ps);
+    }
 }
 
 void launch_prefill_prep(const PrefillArgs& a, hipStream_t s) {
     if (a.B > 64) hipLaunchKernelGGL(prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     if (a.fp8) return;
+    if (a.kcopy) {
+        if (a.D == 128) hipLaunchKernelGGL(kv4copy_kernel<128>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(kv4copy_kernel<64>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
+        return;
+    }
     if (a.D == 128) hipLaunchKernelGGL(vcopy_kernel<128>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
     else hipLaunchKernelGGL(vcopy_kernel<64>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
 }
@@ -1196,15 +1755,20 @@ void launch_prefill_prep(const PrefillArgs& a, hipStream_t s) {
 void launch_prefill_attn(const PrefillArgs& a, hipStream_t s) {
     constexpr int NH = kPrefillKeys / 32;
     const dim3 grid((unsigned)((a.max_units + kXcds - 1) / kXcds * kXcds));
-    if (a.fp8) {
+    if (a.kcopy) {
         if (a.D == 128)
-            hipLaunchKernelGGL((prefill_attn_kernel<128, NH, true>), grid, dim3(256), 0, s, a);
+            hipLaunchKernelGGL((prefill_attn_kernel<128, NH, false, true>), grid, dim3(256), 0, s, a);
         else
-            hipLaunchKernelGGL((prefill_attn_kernel<64, NH, true>), grid, dim3(256), 0, s, a);
+            hipLaunchKernelGGL((prefill_attn_kernel<64, NH, false, true>), grid, dim3(256), 0, s, a);
+    } else if (a.fp8) {
+        if (a.D == 128)
+            hipLaunchKernelGGL((prefill_attn_kernel<128, NH, true, false>), grid, dim3(256), 0, s, a);
+        else
+            hipLaunchKernelGGL((prefill_attn_kernel<64, NH, true, false>), grid, dim3(256), 0, s, a);
     } else if (a.D == 128) {
-        hipLaunchKernelGGL((prefill_attn_kernel<128, NH, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((prefill_attn_kernel<128, NH, false, false>), grid, dim3(256), 0, s, a);
     } else {
-        hipLaunchKernelGGL((prefill_attn_kernel<64, NH, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((prefill_attn_kernel<64, NH, false, false>), grid, dim3(256), 0, s, a);
     }
     if (!a.split) return;
     // a wave for every 32 rows x 32 dims of a tile

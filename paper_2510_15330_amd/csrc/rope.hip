@@ -1,0 +1,169 @@
+// Norm and rotation of queries and keys, before they enter the cache and the
+// attention: y = R(p) (x / sqrt(mean(x^2) + eps) * (w + offset)) per head row,
+// R(p) turning each pair of the first R dims by position times frequency.
+//
+// Bound by memory: (H_q + H_kv) D values a token read and written once.  A row
+// is D / 16 lanes, each with two 16-byte units whose values pair up (dims i and
+// i + R / 2, or neighbours), so nothing crosses lanes but the sum of squares; a
+// wave walks a token's rows, 64 / (D / 16) at a time, queries first.  A lane's
+// eight angles are the same for all rows of the token: they are formed once a
+// wave, in turns, the product in binary64 (a position of 2^20 times a frequency
+// near 1 is exact to 2^-29 turns there, to 2^-3 in binary32), its fraction to
+// the sine and cosine units, which take turns (measured within 1.3e-7).
+// Everything between the loads and the rounding to bf16 is binary32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "internal.h"
+
+namespace bellman {
+namespace {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void widen8(const u32x4& u, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ u32x4 round8(const float* y) {
+    u32x4 u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 v = {y[2 * i], y[2 * i + 1]};
+        u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));   // nearest even
+    }
+    return u;
+}
+
+// Sum over the LPR (4 or 8) neighbouring lanes of a row.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));   // lane ^ 1
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));   // lane ^ 2
+    if (LPR == 8)
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));   // half mirror
+    return v;
+}
+
+template <int D, bool INTER>
+__global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a) {
+    constexpr int LPR = D / 16, RPW = 64 / LPR;     // lanes a row, rows a pass
+    const int lane = threadIdx.x & 63, j = lane % LPR, sub = lane / LPR;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = id / a.chunks;
+    if (t >= a.T) return;
+    const int c = (int)(id - t * a.chunks);
+    const int pq = (a.H_q + RPW - 1) / RPW, passes = pq + (a.H_kv + RPW - 1) / RPW;
+    const int p0 = passes * c / a.chunks, p1 = passes * (c + 1) / a.chunks;
+
+    // this lane's units; the first R / 16 lanes of a row rotate theirs
+    const bool turns = j < a.R / 16;
+    const int ua = !INTER && turns ? 8 * j : 16 * j, ub = !INTER && turns ? 8 * j + a.R / 2 : 16 * j + 8;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        cs[i] = 1.f;
+        sn[i] = 0.f;
+    }
+    if (turns) {
+        int pos[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) pos[x] = a.positions[min(x, a.axes - 1) * a.pos_stride + t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int f = 8 * j + i;
+            const int p = f < a.cut[0] ? pos[0] : f < a.cut[1] ? pos[1] : f < a.cut[2] ? pos[2] : pos[3];
+            const double r = (double)p * (double)a.inv_freq[f] * 0.15915494309189535;   // 1 / (2 pi)
+            const float turn = (float)(r - __builtin_rint(r));
+            cs[i] = __builtin_amdgcn_cosf(turn);
+            sn[i] = __builtin_amdgcn_sinf(turn);
+        }
+    }
+    float w[16];
+    int have = -1;         // whose weights w holds: 0 queries, 1 keys
+    for (int p = p0; p < p1; ++p) {
+        const bool isk = p >= pq;
+        const int H = isk ? a.H_kv : a.H_q;
+        const int row = (isk ? p - pq : p) * RPW + sub, h = min(row, H - 1);
+        const uint16_t* src = isk ? a.k + t * a.k_st + (int64_t)h * a.k_sh : a.q + t * a.q_st + (int64_t)h * a.q_sh;
+        const u32x4 xa = *(const u32x4*)(src + ua), xb = *(const u32x4*)(src + ub);
+        const void* wp = isk ? a.k_weight : a.q_weight;
+        if (wp && have != (int)isk) {
+            have = (int)isk;
+            if (isk ? a.kw_fp32 : a.qw_fp32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    w[i] = ((const float*)wp)[ua + i] + a.offset;
+                    w[8 + i] = ((const float*)wp)[ub + i] + a.offset;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    w[i] = __uint_as_float((uint32_t)((const uint16_t*)wp)[ua + i] << 16) + a.offset;
+                    w[8 + i] = __uint_as_float((uint32_t)((const uint16_t*)wp)[ub + i] << 16) + a.offset;
+                }
+            }
+        }
+        float x[16];
+        widen8(xa, x);
+        widen8(xb, x + 8);
+        if (wp) {
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
+            const float inv = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + a.eps);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = x[i] * inv * w[i];
+        }
+        u32x4 ya, yb;
+        if (turns) {
+            float y[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // the pair of frequency 8 j + i
+                const int e = INTER ? 2 * i : i, o = INTER ? 2 * i + 1 : i + 8;
+                y[e] = __builtin_fmaf(x[e], cs[i], -(x[o] * sn[i]));
+                y[o] = __builtin_fmaf(x[o], cs[i], x[e] * sn[i]);
+            }
+            ya = round8(y);
+            yb = round8(y + 8);
+        } else {
+            ya = round8(x);
+            yb = round8(x + 8);
+        }
+        if (row < H) {
+            uint16_t* dst = isk ? a.k_out + t * a.ko_st + (int64_t)h * a.ko_sh : a.q_out + t * a.qo_st + (int64_t)h * a.qo_sh;
+            *(u32x4*)(dst + ua) = ya;
+            *(u32x4*)(dst + ub) = yb;
+        }
+    }
+}
+
+}  // namespace
+
+void launch_qk_norm_rope(const RopeArgs& args, hipStream_t s) {
+    RopeArgs a = args;
+    const int rpw = 64 / (a.D / 16);
+    const int passes = (a.H_q + rpw - 1) / rpw + (a.H_kv + rpw - 1) / rpw;
+    // A token's passes go over as many waves as it takes to have 8192 (eight a
+    // SIMD); from 8192 tokens on one wave takes a token and forms its angles once.
+    a.chunks = (int)std::min<int64_t>(passes, (8192 + a.T - 1) / a.T);
+    const dim3 grid((unsigned)(((int64_t)a.T * a.chunks + 3) / 4));
+    if (a.D == 128) {
+        if (a.interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((qk_norm_rope_kernel<128, false>), grid, dim3(256), 0, s, a);
+    } else {
+        if (a.interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<64, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((qk_norm_rope_kernel<64, false>), grid, dim3(256), 0, s, a);
+    }
+}
+
+}  // namespace bellman
