@@ -198,7 +198,8 @@ int check_pools4(const bellman_tensor_t* k, const bellman_tensor_t* v, PoolShape
                         (long long)k->shape[i]);
     const int64_t half = k->shape[3];
     if (half != 32 && half != 64) return fail(BELLMAN_ERR_UNSUPPORTED, "head_dim %lld: only 64 and 128 are supported", (long long)(2 * half));
-    if (k->shape[1] < 1 || k->shape[1] > INT32_MAX) return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: %lld KV heads", (long long)k->shape[1]);
+    if (k->shape[1] < 1) return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: no KV heads");
+    if (k->shape[1] > 65535) return fail(BELLMAN_ERR_UNSUPPORTED, "4-bit pools of more than 65535 KV heads");
     if (k->shape[0] < 1) return fail(BELLMAN_ERR_INVALID_ARG, "k_pages: the pool has no pages");
     if (k->shape[0] > INT32_MAX) return fail(BELLMAN_ERR_UNSUPPORTED, "more than 2^31-1 pages");
     if (!is_contiguous(k)) return fail(BELLMAN_ERR_UNSUPPORTED, "k_pages: must be contiguous");

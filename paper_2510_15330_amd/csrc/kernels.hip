@@ -8,6 +8,7 @@
 #include "wave_scan.h"
 #include "work_split.h"
 
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -257,6 +258,13 @@ struct PageV {
 template <typename T>
 __device__ __forceinline__ T ld_stream(const char* p) {
     return __builtin_nontemporal_load((const T*)p);
+}
+// the same at a scalar base address (a generic pointer made from it would load
+// through the flat path)
+typedef const __attribute__((address_space(1))) char* global_ptr;
+template <typename T>
+__device__ __forceinline__ T ld_stream_at(uint64_t base, uint32_t off) {
+    return __builtin_nontemporal_load((const __attribute__((address_space(1))) T*)((global_ptr)base + off));
 }
 
 template <int D, bool FP8>
@@ -711,7 +719,10 @@ __device__ __forceinline__ void fp8_step(AttnState<D>& st, const PageK<D, true> 
 // as large (their reference is 127 below the running max), so a scaled
 // weight's bf16 bits are the weight's less (254 - s) << 7, one saturating 16-bit
 // subtraction for two values; what falls below 2^-126 becomes 0 or below
-// 2^-126.  All lanes of a group read the same 16 scale bytes of a page.
+// 2^-126.  Each lane loads four of the step's V scale bytes and forms their
+// subtrahends; the lanes of a slot group then read theirs from LDS (a load of
+// all a lane's 64 scale bytes instead took 4 more KiB through the cache, 16
+// more registers a step in flight and 75 more instructions a step).
 template <int D, int PP>
 struct Page4 {
     static constexpr int NK = D == 128 ? PP : PP / 2;   // 16-byte K loads a lane
@@ -719,9 +730,16 @@ struct Page4 {
     u32x4 k[NK];
     uint32_t ks[NK];      // the scale byte of k
     VT v[PP];             // dword b: tiles 2b, 2b + 1 (dims 32 b + n, 32 b + 16 + n), slots 4qg..4qg+3
-    VT vs[PP];            // dword b: the scales of block b, slots 4qg..4qg+3
-    uint32_t chk;         // page qg: dword n (head_dim 64: n mod 8) of its V scales
+    uint32_t vs;          // page qg: dword n (head_dim 64: n mod 8) of its V scales
 };
+
+// This wave's subtrahends in LDS: pairs (slots 0, 1; slots 2, 3) of dword n of
+// page i's V scales at [i][n], that is [i][slot group][block].
+template <int D>
+__device__ __forceinline__ u32x4* sub_store() {
+    __shared__ u32x4 s[kAttnBlock / kWaveSize][4 * D / 16];
+    return s[threadIdx.x >> 6];
+}
 
 // The query terms as B operands: [0] (and at head_dim 64 [1], moved to the
 // upper k half for the odd pages).
@@ -730,10 +748,14 @@ struct Q4 {
     i32x8 hi[D == 128 ? 1 : 2], lo[D == 128 ? 1 : 2];
     int s_hi, s_lo;
 };
+// flip: the sign bits that a negative softmax scale turns
 template <int D>
-__device__ __forceinline__ void q_to_fp4(const bf16x8 (&bq)[D / 32], Q4<D>& q4) {
+__device__ __forceinline__ void q_to_fp4(const bf16x8 (&bq)[D / 32], Q4<D>& q4, uint32_t flip) {
+    bf16x8 q[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) q[j] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, bq[j]) ^ flip);
     Q8 q8;
-    q_to_fp8<D>(bq, q8);
+    q_to_fp8<D>(q, q8);
     q4.hi[0] = q8.hi;
     q4.lo[0] = q8.lo;
     if constexpr (D == 64) {
@@ -766,12 +788,30 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t p, uint32_t sub) {
 constexpr float kRef4 = 127.f;                 // the weights' reference below the max, log2
 constexpr uint32_t kDenorm127 = 0x00400000u;   // 2^-127
 
-// One step of PP = 4 pages: nv[i] slots of page i count, full: all do.
+// One step of PP = 4 pages: nv[i] slots of page i count, full: all do.  sl is
+// the softmax scale's magnitude (above 0), in log2 units.
 template <int D, int PP>
 __device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, const Q4<D>& q4, float sl,
                                          const int (&nv)[PP], int qg, int n, bool full) {
-    static_assert(PP == 4, "four pages, one a lane group in the scale check");
+    static_assert(PP == 4, "four pages, one a lane group in the scales");
     constexpr int NT = D / 16, NB = D / 32;
+    // the subtrahends (254 - s) << 7 of this lane's four scales, to LDS, and
+    // this lane group's back (a 255 borrows from its later neighbours: they
+    // are of its block, which is NaN, or past the length)
+    u32x4* sub = sub_store<D>();
+    {
+        const uint32_t y = 0xfefefefeu - pg.vs;
+        const u32x2 s = {__builtin_amdgcn_perm(0u, y, 0x010c000cu) >> 1, __builtin_amdgcn_perm(0u, y, 0x030c020cu) >> 1};
+        ((u32x2*)sub)[D / 8 * qg + (n & (D / 8 - 1))] = s;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    u32x4 su[PP][NB / 2];     // [page][b / 2]: blocks b, b + 1
+#pragma unroll
+    for (int i = 0; i < PP; ++i)
+#pragma unroll
+        for (int b = 0; b < NB / 2; ++b) su[i][b] = sub[D / 16 * i + NB / 2 * qg + b];
     if constexpr (D == 64) {
         // a dead slot's scale may be a NaN, which would reach the other page's
         // sums through its zero query terms
@@ -793,10 +833,11 @@ __device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, con
         s4 = mfma_f4(pg.k[j], (int)pg.ks[j], q4.hi[h], q4.s_hi, s4);
         s4 = mfma_f4(pg.k[j], (int)pg.ks[j], q4.lo[h], q4.s_lo, s4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[4 * i + r] = s4[r] * sl;
+        for (int r = 0; r < 4; ++r) x[4 * i + r] = s4[r];
     }
-    uint32_t chk = pg.chk;
+    uint32_t chk = pg.vs;
     if (!full) {
+        asm volatile("" ::: "memory");      // stays a branch
 #pragma unroll
         for (int i = 0; i < PP; ++i)
 #pragma unroll
@@ -807,7 +848,7 @@ __device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, con
 #pragma unroll
     for (int i = 0; i < 4 * PP; ++i) mx = fmaxf(mx, x[i]);
     mx = group_max4(mx);
-    const float m_new = fmaxf(st.m, mx - kRef4);
+    const float m_new = fmaxf(st.m, __builtin_fmaf(mx, sl, -kRef4));
     if (__any(m_new > st.m)) {
         const float alpha = fast_exp2(st.m - m_new);
         st.l *= alpha;
@@ -830,7 +871,7 @@ __device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, con
     float psum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4 * PP; i += 2) {
-        const float p0 = fast_exp2(x[i] - st.m), p1 = fast_exp2(x[i + 1] - st.m);
+        const float p0 = fast_exp2(__builtin_fmaf(x[i], sl, -st.m)), p1 = fast_exp2(__builtin_fmaf(x[i + 1], sl, -st.m));
         psum = __builtin_fmaf(p0, __uint_as_float(kDenorm127), psum);
         psum = __builtin_fmaf(p1, __uint_as_float(kDenorm127), psum);
         const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
@@ -847,11 +888,8 @@ __device__ __forceinline__ void fp4_step(AttnState<D>& st, Page4<D, PP>& pg, con
             u32x4 bh, bl;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                // (254 - s) << 7 of the four slots (a 255 borrows from its
-                // neighbours: the block is NaN already)
-                const uint32_t y = 0xfefefefeu - pg.vs[2 * j + e][b];
-                const uint32_t s01 = __builtin_amdgcn_perm(0u, y, 0x010c000cu) >> 1;
-                const uint32_t s23 = __builtin_amdgcn_perm(0u, y, 0x030c020cu) >> 1;
+                const u32x4 w = su[2 * j + e][b / 2];
+                const uint32_t s01 = b & 1 ? w.z : w.x, s23 = b & 1 ? w.w : w.y;
                 bh[2 * e] = scaled_pair(ph[4 * j + 2 * e], s01);
                 bh[2 * e + 1] = scaled_pair(ph[4 * j + 2 * e + 1], s23);
                 bl[2 * e] = scaled_pair(pl[4 * j + 2 * e], s01);
@@ -1252,7 +1290,7 @@ attn_mfma_kernel(AttnArgs a) {
     auto bt_load = [&](const Cursor& c) -> int {
         // page i of the step sits in lane i, or in lane group i when fp8 V
         // rows are read by page (each lane then addresses its own page)
-        constexpr bool kRows = FP8 && PP == 4;
+        constexpr bool kRows = (FP8 || FP4) && PP == 4;
         const int i = kRows ? (lane >> 4) : PP == 1 ? (lane & 1) : (lane & (PP - 1));
         const int idx = min(c.p + i, (PP == 1 ? c.np : c.p + c.len) - 1);
         return a.block_table[(int64_t)c.b * a.bt_stride + idx];
@@ -1261,7 +1299,16 @@ attn_mfma_kernel(AttnArgs a) {
     // head g*G + n.  Lanes n >= G hold a copy of the group's last head; their
     // columns of S and O are computed and discarded, which keeps this load
     // free of lane masks.
+    const uint64_t q_lane = (uint64_t)(a.q + (int64_t)min(n, a.G - 1) * a.q_sh + 16 * qg);   // 4-bit pools
     auto q_load = [&](const Cursor& c, bf16x8 (&bq)[KS]) {
+        if constexpr (FP4) {
+            uint64_t at = 2 * ((uint64_t)c.b * (uint64_t)a.q_sb + (uint64_t)(uint32_t)(c.g * a.G) * (uint64_t)a.q_sh);
+            asm("" : "+s"(at));
+            const auto* row = (const __attribute__((address_space(1))) u32x4*)(q_lane + at);
+#pragma unroll
+            for (int j = 0; j < KS; ++j) bq[j] = __builtin_bit_cast(bf16x8, row[(j & 1) + 8 * (j >> 1)]);
+            return;
+        }
         const uint16_t* qrow = a.q + (int64_t)c.b * a.q_sb + (int64_t)(c.g * a.G + min(n, a.G - 1)) * a.q_sh;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -1300,44 +1347,45 @@ attn_mfma_kernel(AttnArgs a) {
         }
     };
 
+    // 4-bit pools: lane group qg finds page qg's tile; the pages' addresses then
+    // go into scalar registers.  They and the lane's 32-bit offsets are opaque to
+    // the compiler, which otherwise hoists a 64-bit vector address out of the
+    // loop and adds the page to it load by load.
     auto kv4_load = [&](const Cursor& c, int btv, Page4<D, 4>& r, bool& bad) {
-        bad = false;
-        size_t off[4];
+        const bool ok = (unsigned)btv < (unsigned)a.num_pages;
+        bad = __ballot(!ok) != 0;
+        bad_pages |= bad;
+        const uint64_t own = (uint64_t)(unsigned)(ok ? btv : 0) * (uint32_t)page_stride + (uint32_t)c.g * (uint32_t)tile_bytes;
+        uint64_t kb[4], vb[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            int pg = __builtin_amdgcn_readlane(btv, i);
-            if ((unsigned)pg >= (unsigned)a.num_pages) {
-                pg = 0;
-                bad = true;
-                bad_pages = 1;
-            }
-            off[i] = (size_t)pg * page_stride + (size_t)c.g * tile_bytes;
+            const uint64_t off = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)own, 16 * i) |
+                                 (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(own >> 32), 16 * i) << 32;
+            kb[i] = (uint64_t)a.k_pages + off;
+            vb[i] = (uint64_t)a.v_pages + off;
+            asm("" : "+s"(kb[i]), "+s"(vb[i]));
         }
-        const char* kp = (const char*)a.k_pages;
-        const char* vp = (const char*)a.v_pages;
+        uint32_t k_off = (D == 128 ? lane : lane & 31) * 16, s_off = D == 128 ? lane : lane & 31, v_off = lane * (D / 8);
+        asm volatile("" : "+v"(k_off), "+v"(s_off), "+v"(v_off));
         if constexpr (D == 128) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                r.k[i] = ld_stream<u32x4>(kp + off[i] + (size_t)(lane * 16));
-                r.ks[i] = ld_stream<uint8_t>(kp + off[i] + (size_t)(8 * D + lane));
+                r.k[i] = ld_stream_at<u32x4>(kb[i], k_off);
+                r.ks[i] = ld_stream_at<uint8_t>(kb[i] + 8 * D, s_off);
             }
         } else {
             // lane groups 0, 1: the pair's first page; 2, 3: its second
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const char* tile = kp + (lane < 32 ? off[2 * j] : off[2 * j + 1]);
-                r.k[j] = ld_stream<u32x4>(tile + (size_t)((lane & 31) * 16));
-                r.ks[j] = ld_stream<uint8_t>(tile + (size_t)(8 * D + (lane & 31)));
+                const uint64_t tile = lane < 32 ? kb[2 * j] : kb[2 * j + 1];
+                r.k[j] = ld_stream_at<u32x4>(tile, k_off);
+                r.ks[j] = ld_stream_at<uint8_t>(tile + 8 * D, s_off);
             }
         }
         using VT = typename Page4<D, 4>::VT;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            r.v[i] = ld_stream<VT>(vp + off[i] + (size_t)(lane * (D / 8)));
-            r.vs[i] = ld_stream<VT>(vp + off[i] + (size_t)(8 * D + qg * (D / 8)));
-        }
-        const size_t own = qg == 0 ? off[0] : qg == 1 ? off[1] : qg == 2 ? off[2] : off[3];
-        r.chk = ld_stream<uint32_t>(vp + own + (size_t)(8 * D + 4 * (n & (D / 8 - 1))));
+        for (int i = 0; i < 4; ++i) r.v[i] = ld_stream_at<VT>(vb[i], v_off);
+        r.vs = ld_stream<uint32_t>((const char*)a.v_pages + own + 8 * D + 4 * (n & (D / 8 - 1)));
     };
 
     // m starts at the lowest finite value: scores of -inf alone weigh nothing
@@ -1429,7 +1477,7 @@ attn_mfma_kernel(AttnArgs a) {
         if constexpr (FP4) kv4_load(cur[DEPTH], btn, pb[ld_], badb[ld_]);
         else kv_load(cur[DEPTH], btn, kb[ld_], vb[ld_], badb[ld_]);
         btn = btT;
-        if constexpr ((FP8 || FP4) && DEPTH > 1) consume(qb[sc_]);
+        if constexpr (FP8 && DEPTH > 1) consume(qb[sc_]);
 
         const Cursor& C = cur[0];
         float sl = a.scale_log2, vs = 1.f;
@@ -1440,14 +1488,14 @@ attn_mfma_kernel(AttnArgs a) {
         seg_bad = seg_bad || badb[sc_];
         if constexpr (FP4) {
             if (C.b != q8_b || C.g != q8_g) {
-                q_to_fp4<D>(qb[sc_], q4);
+                q_to_fp4<D>(qb[sc_], q4, a.scale_log2 < 0.f ? 0x80008000u : 0u);
                 q8_b = C.b;
                 q8_g = C.g;
             }
             int nv[PP];
 #pragma unroll
             for (int i = 0; i < PP; ++i) nv[i] = (i == 0 || C.len > i) ? min(kPage, C.L - (C.p + i) * kPage) : 0;
-            fp4_step<D, PP>(st, pb[sc_], q4, sl, nv, qg, n, C.len == PP && C.L >= (C.p + PP) * kPage);
+            fp4_step<D, PP>(st, pb[sc_], q4, fmaxf(fabsf(sl), FLT_MIN), nv, qg, n, C.len == PP && C.L >= (C.p + PP) * kPage);
         } else if constexpr (FP8) {
             if (C.b != q8_b || C.g != q8_g) {  // new (request, head): convert its query rows
                 q_to_fp8<D>(qb[sc_], q8);
