@@ -150,7 +150,8 @@ int bellman_kv_append(const bellman_tensor_t *k_new, const bellman_tensor_t *v_n
  *   scale        finite fp32 softmax scale (usually 1/sqrt(D)).
  *   out          bf16 [B, H_q, D], innermost contiguous (written; rounded to
  *                nearest even).  A request of length 0 gets zeros.
- * Over 4-bit pools the keys enter the matrix cores as they lie; the values'
+ * Over 4-bit pools the keys enter the matrix cores as they lie (a score is off
+ * by at most 2^-13 of its sum of |products|); the values'
  * scales go into the weights, held as the sum of two bf16 (2^-14 relative),
  * whose scaled magnitudes below 2^-126 count as 0.  A NaN key block makes its
  * (request, head)'s rows NaN, a NaN value block its 32 dims of them.
@@ -183,7 +184,7 @@ typedef struct bellman_attn_opts {
                              the GPU can keep resident, but where pages_per_step
                              and pipeline_depth are 0 too one workgroup of four
                              waves per CU over bf16 pools, and one or two by the
-                             call's shape over fp8 pools.  Fewer waves split fewer
+                             call's shape over fp8 and 4-bit pools.  Fewer waves split fewer
                              requests (results agree within rounding). */
     int32_t xcd_skew;     /* share weights of the waves of even- and odd-numbered
                              XCDs (workgroup i runs on XCD i mod 8), applied only
@@ -249,9 +250,9 @@ int bellman_decode_attention_opts(const bellman_tensor_t *q, const bellman_tenso
  * ends, instead of the growable workspace.  A call needs
  *     256 + 16 W + 8 S + 4 D S   bytes (regions rounded up to 256 B),
  *     S = 2 W G partial slots,
- * W the waves the GPU can hold (1024 for bf16 and 2048 for fp8 pools on a
- * whole MI355X, or max_waves if smaller): up to G = 16 at D = 128 for bf16 pools
- * and G = 8 for fp8 pools by default; fp8 pools with G = 16 need
+ * W the waves the GPU can hold (1024 for bf16 and 2048 for fp8 and 4-bit pools
+ * on a whole MI355X, or max_waves if smaller): up to G = 16 at D = 128 for bf16
+ * pools and G = 8 for the others by default; those with G = 16 need
  * max_waves <= 1900.  A call that needs more is rejected with
  * BELLMAN_ERR_UNSUPPORTED before anything is enqueued.  Every call on one
  * GPU shares that GPU's array and leaves its contents behind (nothing in it

@@ -99,10 +99,11 @@ def write(k_pool, v_pool, k_rows, v_rows, table, lens, new):
 def attention(q, k_pool, v_pool, table, lens, new, scale):
     """Rows of the last new[b] tokens of each request over its keys up to
     their own: (out [T, H_q, D], weights times |values| [T, H_q, D], the
-    magnitude that roundings of weights and scores are relative to)."""
+    magnitude that roundings of weights and scores are relative to, and the
+    largest sum of |products| of a row's scores [T, H_q, 1])."""
     T, H_q, D = q.shape
     H = k_pool.shape[1]
-    out, mag = np.zeros(q.shape), np.zeros(q.shape)
+    out, mag, dot = np.zeros(q.shape), np.zeros(q.shape), np.zeros((T, H_q, 1))
     i = 0
     for b, n in enumerate(new):
         L = int(lens[b])
@@ -118,5 +119,6 @@ def attention(q, k_pool, v_pool, table, lens, new, scale):
             w /= w.sum(-1, keepdims=True)
             out[i:i + n, h] = w @ v[:, g]
             mag[i:i + n, h] = w @ np.abs(v[:, g])
+            dot[i:i + n, h, 0] = (np.abs(q[i:i + n, h]) @ np.abs(k[:, g]).T).max(-1) * abs(scale)
         i += n
-    return out, mag
+    return out, mag, dot

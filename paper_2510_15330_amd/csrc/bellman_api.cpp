@@ -57,7 +57,7 @@ struct Workspace {
 std::mutex g_ws_mutex;
 Workspace g_ws[kMaxDevices];
 int g_cu_count[kMaxDevices];
-int g_blocks_per_cu[kMaxDevices][3][2][5][3];  // [dev][pool type][D==128][pages per step][depth], 0 = unknown
+int g_blocks_per_cu[kMaxDevices][3][2][9][3];  // [dev][pool type][D==128][pages per step][depth], 0 = unknown
 
 int current_device(int* dev) {
     hipError_t e = hipGetDevice(dev);
@@ -363,6 +363,7 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
         return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step 4 is built for fp8 and 4-bit pools only");
     if (ps.fp4 && pps != 0 && pps != 4)
         return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step %d: 4-bit pools take 4 pages a step", pps);
+    if (ps.fp4 && depth == 2) return fail(BELLMAN_ERR_UNSUPPORTED, "pipeline_depth 2 is not built for 4-bit pools");
     const bool chosen = pps == 0 && depth == 0;   // the step is the library's choice
     if (depth == 0) depth = ps.kv == kKvBf16 ? 2 : 1;
     if (B == 0) return BELLMAN_OK;
@@ -435,9 +436,18 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     // 64 of 1-4k 39.0 / 41.5, 41.5 / 43.0 at 8 heads, 43.4 / 42.7 at 16; 20 of
     // 0.5-8k, 77 table pages a wave, 26.9 / 26.2, 28 of them, 108 pages, 31.2 /
     // 31.4 at 4 heads and 34.6 / 32.4 at 8).
-    const bool two = chosen && ps.fp8 &&
-                     (ps.D == 64 ? table_pages_per_wave >= std::max(96.0, 14.0 * (double)G)
-                                 : G <= 8 && table_pages_per_wave >= kWideTablePages);
+    // Over 4-bit pools a step is half an fp8 step's bytes and as many
+    // instructions: at head_dim 64 the second workgroup pays from short shares on
+    // (300 requests of 2-8k 182 / 229 us, 64 of 1-4k 29.5 / 33.8, 20 of 0.5-8k, 78
+    // table pages a wave, 23.7 / 22.4); at head_dim 128 one reads the pages as
+    // fast as two until the shares are long (256 of 6-13.5k 470 / 466 us on one
+    // device, 480 / 492 on another, 512 with Zipf lengths to 8k 194 / 197, 400 of
+    // 3-5k 317 / 318, 64 of 1-4k 43 / 42, 16 heads, 256 of 6-13.5k, 81 / 75).
+    bool two = chosen && ps.fp8 &&
+               (ps.D == 64 ? table_pages_per_wave >= std::max(96.0, 14.0 * (double)G)
+                           : G <= 8 && table_pages_per_wave >= kWideTablePages);
+    if (chosen && ps.fp4)
+        two = ps.D == 64 ? table_pages_per_wave >= 96.0 : G <= 8 && table_pages_per_wave >= 1280.0;
     const int wgs = chosen && !two ? 1 : bpc;
     const int64_t cu_waves = (int64_t)g_cu_count[dev] * (kAttnBlock / kWaveSize);
     int64_t waves = cu_waves * wgs, sized = cu_waves * (depth == asked_depth ? bpc : 1);

@@ -1,13 +1,16 @@
 """4-bit pages on the GPU, against the numpy oracle (oracle/kv4.py).
 
 Writes: bytes of the whole pools, equal.  Reads: values, equal.  Attention:
-element by element |got - ref| <= 2^-8 |ref| + c A, A the oracle's sum of
-weights times |values|: the output's own rounding (bf16, half a step), and what
-the weights and scores are off by relative to A.
-  decode  c = 2^-11: weights hi + lo of truncated bf16 2^-14, their exponent
-          (binary32 scores of magnitude < 64 in log2 units: 64 * 2^-23 * ln 2
-          per rounding, some tens of roundings on the way) below 2^-12
-  prompt  c = 2^-10: the same with weights rounded to fp16 (2^-11 at most)
+element by element |got - ref| <= 2^-8 |ref| + (c + 2^-12 S) A, A the oracle's
+sum of weights times |values|, S its largest sum of |query * key| products of the
+row's scores (scaled): the output's own rounding (bf16, half a step), and what
+weights and scores are off by.
+  c      decode 2^-12: weights as hi + lo of truncated bf16, 2^-14, and the
+         exponent's binary32 roundings; prompt 2^-11: rounded to fp16, 2^-12,
+         and the same
+  2^-12  a score is off by at most 2^-13 of its sum of |products| (the scaled
+         matrix instructions align the products of a few neighbouring dims,
+         keeping 13 bits below the largest); a weight by that and its sum's
 """
 from __future__ import annotations
 
@@ -23,7 +26,7 @@ bl = pytest.importorskip("paper_2510_15330_amd")
 from paper_2510_15330_amd import _binding  # noqa: E402
 
 F4 = torch.float4_e2m1fn_x2
-DECODE, PROMPT = 2.0 ** -11, 2.0 ** -10
+DECODE, PROMPT = 2.0 ** -12, 2.0 ** -11
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -88,11 +91,11 @@ class Cache:
         return [p.view(torch.uint8).cpu().numpy() for p in (self.k, self.v)]
 
 
-def close(got, ref, mag, c, what=""):
+def close(got, ref, mag, dot, c, what=""):
     got = got.detach().float().cpu().double().numpy()
     assert np.array_equal(np.isnan(got), np.isnan(ref)), f"{what}: NaN where none belongs, or none where one does"
     ok = ~np.isnan(ref)
-    off = np.abs(got - ref)[ok] - 2.0 ** -8 * np.abs(ref)[ok] - c * mag[ok]
+    off = np.abs(got - ref)[ok] - 2.0 ** -8 * np.abs(ref)[ok] - ((c + 2.0 ** -12 * dot) * mag)[ok]
     assert not off.size or off.max() <= 0, f"{what}: over the bound by {off.max():.3e}"
 
 
@@ -286,11 +289,11 @@ def test_decode_shapes_and_splits(H_q, H, D, lens):
     rng = np.random.default_rng(H_q + D)
     c = Cache(rng, lens, H, D).to_device()
     qf, q = bf16(rng.standard_normal((len(lens), H_q, D)) * 2)
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * len(lens), D ** -0.5)
-    for kw in ({}, dict(max_waves=1), dict(max_waves=3), dict(max_waves=37), dict(pipeline_depth=2), dict(pages_per_step=4),
-               dict(max_waves=5, pipeline_depth=2)):
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * len(lens), D ** -0.5)
+    for kw in ({}, dict(max_waves=1), dict(max_waves=3), dict(max_waves=37), dict(pages_per_step=4),
+               dict(max_waves=6, pages_per_step=4)):
         out = decode(c, q, D ** -0.5, **kw)
-        close(out, ref, mag, DECODE, f"{kw}")
+        close(out, ref, mag, dot, DECODE, f"{kw}")
         assert torch.equal(out, decode(c, q, D ** -0.5, **kw)), "not the same twice"
     out = torch.empty_like(out)
     # (16 heads of 128 exceed the fixed array at two workgroups a CU: the documented bound)
@@ -308,9 +311,10 @@ def test_decode_random_sweep(seed):
     c = Cache(rng, lens, H, D).to_device()
     qf, q = bf16(rng.standard_normal((B, G * H, D)))
     scale = float(rng.choice([D ** -0.5, 0.0, -0.1, 0.4]))
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * B, scale)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * B, scale)
     for w in (0, 1, int(rng.integers(2, 200))):
-        close(decode(c, q, scale, max_waves=w), ref, mag, DECODE, f"seed {seed} waves {w}")
+        for pp in (0, 4):
+            close(decode(c, q, scale, max_waves=w, pages_per_step=pp), ref, mag, dot, DECODE, f"seed {seed} waves {w} pages {pp}")
 
 
 def test_decode_strided_queries_outputs_and_wide_table():
@@ -324,8 +328,8 @@ def test_decode_strided_queries_outputs_and_wide_table():
     buf = torch.full((B, H_q + 1, D + 8), 9.0, dtype=torch.bfloat16, device="cuda")
     out = buf[:, :H_q, :D]
     bl.decode_attention(q[:, 1:1 + H_q], c.k, c.v, c.bt, c.sl, 0.09, out)
-    ref, mag = kv4.attention(qf[:, 1:1 + H_q], *c.pools, c.table, c.lens, [1] * B, 0.09)
-    close(out, ref, mag, DECODE)
+    ref, mag, dot = kv4.attention(qf[:, 1:1 + H_q], *c.pools, c.table, c.lens, [1] * B, 0.09)
+    close(out, ref, mag, dot, DECODE)
     assert (buf[:, H_q] == 9).all() and (buf[..., D:] == 9).all()
 
 
@@ -355,18 +359,18 @@ def test_nan_blocks(D):
     c.to_device()
     qf, q = bf16(rng.standard_normal((4, G * H, D)))
     with np.errstate(invalid="ignore"):
-        ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 4, 0.1)
+        ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 4, 0.1)
     # the oracle's own NaNs are those: heads 3..5 of request 0, dims 32..63 of heads 0..2 of request 1
     want = np.zeros(ref.shape, dtype=bool)
     want[0, G:] = True
     want[1, :G, 32:64] = True
     assert np.array_equal(np.isnan(ref), want)
-    for kw in ({}, dict(max_waves=1), dict(max_waves=7), dict(pipeline_depth=2)):
-        close(decode(c, q, 0.1, **kw), ref, mag, DECODE, str(kw))
+    for kw in ({}, dict(max_waves=1), dict(max_waves=7), dict(pages_per_step=4)):
+        close(decode(c, q, 0.1, **kw), ref, mag, dot, DECODE, str(kw))
     # the prompt attention over the same pages: keys that a row sees
     out = torch.empty_like(q)
     bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.arange(5, dtype=np.int32)), 0.1, out)
-    close(out, ref, mag, PROMPT)
+    close(out, ref, mag, dot, PROMPT)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -385,23 +389,28 @@ def test_values_of_very_different_sizes(D, spread):
         return x
     c = Cache(rng, lens, H, D, fill=fill).to_device()
     qf, q = bf16(rng.standard_normal((3, G * H, D)) * 3)
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 3, D ** -0.5)
-    for kw in ({}, dict(max_waves=1), dict(max_waves=11)):
-        close(decode(c, q, D ** -0.5, **kw), ref, mag, DECODE, str(kw))
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 3, D ** -0.5)
+    for kw in ({}, dict(max_waves=1), dict(max_waves=11, pages_per_step=4)):
+        close(decode(c, q, D ** -0.5, **kw), ref, mag, dot, DECODE, str(kw))
 
 
 def test_queries_of_very_different_sizes():
-    """Rows from 2^-100 to 2^60: each keeps the scores of its own size."""
+    """Rows from 2^-100 to 2^60 and beyond binary32: each keeps the scores of
+    its own size; the largest finite ones pick one token, infinite ones none."""
     rng = np.random.default_rng(2)
-    H, G, D = 1, 8, 128
+    H, G, D = 1, 9, 128
     c = Cache(rng, [100], H, D).to_device()
-    qf, q = bf16(rng.standard_normal((1, G, D)) * np.exp2([-100, -20, 0, 2, 4, 5, 6, 60])[None, :, None])
+    qf, q = bf16(rng.standard_normal((1, G, D)) * np.exp2([-100, -20, 0, 2, 4, 5, 6, 60, 126])[None, :, None])
     scale = 0.05
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1], scale)
-    out = decode(c, q, scale)
-    # a row of scores up to S (log2 units) is known to S 2^-22: only the first rows' bound holds as stated
-    close(out[:, :6], ref[:, :6], mag[:, :6], DECODE)
-    assert torch.isfinite(out).all()
+    ref, mag, dot = kv4.attention(qf[:, :8], *c.pools, c.table, c.lens, [1], scale)
+    for kw in ({}, dict(max_waves=1), dict(max_waves=3)):
+        out = decode(c, q, scale, **kw)
+        close(out[:, :7], ref[:, :7], mag[:, :7], dot[:, :7], DECODE)
+        close(out[:, 7:8], ref[:, 7:], mag[:, 7:], 0 * dot[:, 7:], DECODE)     # one token's values
+        neg = decode(c, -q, -scale, **kw)
+        assert torch.equal(out[:, :8], neg[:, :8])
+    # the last row's scores overflow binary32 to both infinities
+    assert torch.isnan(out[:, 8]).all()
 
 
 def test_bad_pages_and_lengths():
@@ -415,8 +424,8 @@ def test_bad_pages_and_lengths():
     qf, q = bf16(rng.standard_normal((4, 8, 128)))
     out = decode(c, q, 0.1)
     assert bl.device_errors() == 2 | 4
-    ref, mag = kv4.attention(qf[:1], *c.pools, c.table[:1], want[:1], [1], 0.1)
-    close(out[:1], ref, mag, DECODE)
+    ref, mag, dot = kv4.attention(qf[:1], *c.pools, c.table[:1], want[:1], [1], 0.1)
+    close(out[:1], ref, mag, dot, DECODE)
     assert torch.isnan(out[1:]).all()
 
 
@@ -425,13 +434,13 @@ def test_long_requests_and_many_requests():
     # 30000 tokens on few heads: many waves a request; then 600 short ones
     c = Cache(rng, [30000, 5], 1, 128).to_device()
     qf, q = bf16(rng.standard_normal((2, 8, 128)))
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 128 ** -0.5)
-    close(decode(c, q, 128 ** -0.5), ref, mag, DECODE)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 128 ** -0.5)
+    close(decode(c, q, 128 ** -0.5), ref, mag, dot, DECODE)
     lens = rng.integers(0, 50, 600)
     c = Cache(rng, lens, 2, 64).to_device()
     qf, q = bf16(rng.standard_normal((600, 4, 64)))
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 600, 0.125)
-    close(decode(c, q, 0.125), ref, mag, DECODE)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 600, 0.125)
+    close(decode(c, q, 0.125), ref, mag, dot, DECODE)
 
 
 # ----------------------------------------------------------------- prompt --
@@ -455,9 +464,9 @@ def test_prompt_shapes(H_q, H, D, cached, new):
     qs = dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
     out = torch.empty_like(q)
     for scale in (D ** -0.5, -0.05):
-        ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, new, scale)
+        ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, new, scale)
         bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, qs, scale, out)
-        close(out, ref, mag, PROMPT, f"scale {scale}")
+        close(out, ref, mag, dot, PROMPT, f"scale {scale}")
     assert bl.device_errors() == 0
 
 
@@ -468,8 +477,8 @@ def test_prompt_many_requests():
     qf, q = bf16(rng.standard_normal((int(new.sum()), 4, 64)))
     out = torch.empty_like(q)
     bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), 0.125, out)
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, new, 0.125)
-    close(out, ref, mag, PROMPT)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, new, 0.125)
+    close(out, ref, mag, dot, PROMPT)
 
 
 def test_prompt_page_outside_the_pool():
@@ -481,8 +490,8 @@ def test_prompt_page_outside_the_pool():
     out = torch.empty_like(q)
     bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.array([0, 64, 128], dtype=np.int32)), 0.1, out)
     assert bl.device_errors() == 4
-    ref, mag = kv4.attention(qf[64:], *c.pools, c.table[1:], c.lens[1:], [64], 0.1)
-    close(out[64:], ref, mag, PROMPT)
+    ref, mag, dot = kv4.attention(qf[64:], *c.pools, c.table[1:], c.lens[1:], [64], 0.1)
+    close(out[64:], ref, mag, dot, PROMPT)
     assert torch.isnan(out[32:64]).all() and not torch.isnan(out[:32]).any()
 
 
@@ -497,8 +506,8 @@ def test_prompt_values_of_different_sizes(spread):
     qf, q = bf16(rng.standard_normal((100, 2, 128)))
     out = torch.empty_like(q)
     bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.array([0, 100], dtype=np.int32)), 0.1, out)
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [100], 0.1)
-    close(out, ref, mag, PROMPT)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [100], 0.1)
+    close(out, ref, mag, dot, PROMPT)
 
 
 # --------------------------------------------------------- used together --
@@ -612,8 +621,8 @@ def test_prompt_then_decode_run():
             bl.kv_write(ko, v, c.k, c.v, c.bt, c.sl, qs)
             bl.prefill_attention(qo, c.k, c.v, c.bt, c.sl, qs, D ** -0.5, out)
         kv4.write(*c.pools, ko.double().cpu().numpy(), xf[:, -H:], c.table, c.lens, new)
-        ref, mag = kv4.attention(qo.double().cpu().numpy(), *c.pools, c.table, c.lens, new, D ** -0.5)
-        close(out, ref, mag, DECODE if new == [1, 1] else PROMPT)
+        ref, mag, dot = kv4.attention(qo.double().cpu().numpy(), *c.pools, c.table, c.lens, new, D ** -0.5)
+        close(out, ref, mag, dot, DECODE if new == [1, 1] else PROMPT)
     assert all(np.array_equal(a, b) for a, b in zip(c.bytes(), c.pools)) and bl.device_errors() == 0
 
 
@@ -630,5 +639,5 @@ def test_another_stream():
     bl.decode_attention(q, c.k, c.v, c.bt, c.sl, 0.1, out, stream=st)
     st.synchronize()
     kv4.write(*c.pools, kf, kf, c.table, c.lens, [1, 1])
-    ref, mag = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 0.1)
-    close(out, ref, mag, DECODE)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 0.1)
+    close(out, ref, mag, dot, DECODE)

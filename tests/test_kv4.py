@@ -92,12 +92,12 @@ def test_oracle_attention_is_the_dense_softmax():
     k, v = rng.standard_normal((21, H, D)), rng.standard_normal((21, H, D))
     kv4.write(*pools, k, v, table, lens, [21])
     q = rng.standard_normal((4, H * G, D))
-    out, mag = kv4.attention(q, *pools, table, lens, [4], 0.125)
+    out, mag, dot = kv4.attention(q, *pools, table, lens, [4], 0.125)
     kd, vd = (kv4.dequantize(*kv4.quantize(x)) for x in (k, v))
     for i in range(4):
         ref = dense_attention(q[i], kd[:18 + i], vd[:18 + i], 0.125)
         assert np.abs(out[i] - ref).max() < 1e-12
-    assert (mag >= np.abs(out) - 1e-12).all()
+    assert (mag >= np.abs(out) - 1e-12).all() and (dot > 0).all()
 
 
 def test_oracle_rotation_against_complex_numbers():
