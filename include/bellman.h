@@ -412,14 +412,14 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * (values more than 2^63 below the largest of a key range lose bits).  Over fp8 pools the
  * codes are staged in LDS as bytes and widened exactly at the operand load
  * (K to bf16, V to fp16); the K scale folds into the softmax scale and the
- * V scale into the final normalisation.  Over 4-bit pools the keys the call
- * reads are copied too, widened exactly to bf16, and the values to fp16 as over
+ * V scale into the final normalisation.  Over 4-bit pools the keys enter the
+ * matrix cores as they lie, against the query as two e4m3 terms (scores as in the
+ * decode attention), and the values are copied to fp16 as over
  * bf16 pools; a page outside the pool makes the rows that see it NaN.  Scratch
  * in the per-device
- * workspace: 3 KiB + 4 (B + 1) bytes; over bf16 pools, for the value copy
- * and its bookkeeping, B ceil(maxP / 4) (4 + 4 H_kv + 128 D H_kv) +
- * 4 (B + 1) bytes more (maxP = the block table's width), over 4-bit pools
- * B ceil(maxP / 4) 128 D H_kv more than that; and where keys are
+ * workspace: 3 KiB + 4 (B + 1) bytes; over bf16 and 4-bit pools, for the
+ * value copy and its bookkeeping, B ceil(maxP / 4) (4 + 4 H_kv + 128 D H_kv) +
+ * 4 (B + 1) bytes more (maxP = the block table's width); and where keys are
  * shared out 128 (4 D + 8) bytes a share, at most four shares a CU (a capture
  * with no room for those, or a call whose device has no memory for them, runs
  * uncut; results agree within rounding).  Like

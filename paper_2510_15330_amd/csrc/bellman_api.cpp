@@ -946,7 +946,7 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
         return fail(BELLMAN_ERR_UNSUPPORTED, "too many query tiles x heads");
     if (T == 0 || B == 0) return BELLMAN_OK;
 
-    // bf16 pools: the fp16 copy of the values holds at most every table page
+    // bf16 and 4-bit pools: the fp16 copy of the values holds at most every table page
     // of every request (B x maxP pages of H_kv heads)
     const int64_t max_pages = block_table->shape[1];
     const size_t page_head_bytes = (size_t)ps.D * 16 * 2;
@@ -982,9 +982,7 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     const size_t off_req = off_steps + align256(planned && !ps.fp8 ? (size_t)(B + 1) * 4 : 0);
     const size_t off_exp = off_req + align256(planned && !ps.fp8 ? max_steps * 4 : 0);
     const size_t off_copy = off_exp + align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4);
-    const size_t copy_bytes = align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4 * page_head_bytes);
-    const size_t off_kcopy = off_copy + copy_bytes;      // 4-bit pools: the keys' copy
-    const size_t off_ml = off_kcopy + (ps.fp4 ? copy_bytes : 0);
+    const size_t off_ml = off_copy + align256(ps.fp8 ? 0 : max_steps * ps.H_kv * 4 * page_head_bytes);
     const size_t piece_rows = a.split ? (size_t)a.max_units * kPrefillRows : 0;
     const size_t off_o = off_ml + align256(piece_rows * sizeof(float2));
     const size_t total = off_o + align256(piece_rows * ps.D * sizeof(float));
@@ -1032,6 +1030,7 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     a.err = err;
     a.tile_start = (int32_t*)(base + off_tiles);
     a.fp8 = ps.fp8 ? 1 : 0;
+    a.fp4 = ps.fp4 ? 1 : 0;
     a.k_scale = k_pages->dequant_scale;
     a.v_scale = v_pages->dequant_scale;
     a.chunk = (int32_t*)(base + off_chunk);
@@ -1041,7 +1040,6 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     a.step_req = (int32_t*)(base + off_req);
     a.vexp = (int32_t*)(base + off_exp);
     a.vcopy = (uint16_t*)(base + off_copy);
-    a.kcopy = ps.fp4 ? (uint16_t*)(base + off_kcopy) : nullptr;
     // a workgroup for every (step, head) tile of B x maxP pages at most once,
     // and at most 4096
     a.vgrid = (int)std::max<int64_t>(1, std::min<int64_t>(4096, (int64_t)max_steps * ps.H_kv));

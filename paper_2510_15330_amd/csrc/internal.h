@@ -131,6 +131,7 @@ struct PrefillArgs {
     int B, T, H_q, H_kv, G, D, max_pages;
     int32_t* err;
     int fp8;               // pools of e4m3fn codes with the dequantisation scales below
+    int fp4;               // 4-bit pools
     const float* k_scale;  // fp8 only, fp32 [B, H_kv]
     const float* v_scale;
     int64_t max_tiles;     // no more (tile, KV head)s, and no more units, than these
@@ -142,12 +143,11 @@ struct PrefillArgs {
     int32_t* chunk;        // steps of a key-split unit, written by the attention for the merge
     float2* part_ml;       // [max_units, 128]: (running max in log2 units, sum) of each row of a piece
     float* part_o;         // [max_units, 128 D]: its normalised output, in lane order
-    // bf16 pools: the fp16 copy of the values the attention reads
+    // bf16 and 4-bit pools: the fp16 copy of the values the attention reads
     int32_t* step_off;     // [B + 1]: first copied 64-key step of each request (B > 64)
     int32_t* step_req;     // [B * ceil(maxP / 4)]: the request of each copied step (B > 64)
     int32_t* vexp;         // [copied steps, H_kv]: the exponent of the step's scale
     uint16_t* vcopy;       // [copied steps, H_kv, 4 pages, D, 16] fp16
-    uint16_t* kcopy;       // 4-bit pools: the keys as bf16, [copied steps, H_kv, 4 pages, D/8, 16, 8]; else null
     int vgrid;             // workgroups of the copy
 };
 

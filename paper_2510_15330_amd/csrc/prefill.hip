@@ -30,6 +30,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ float swap_halves(float x) {  // value of lane l ^ 32
     const unsigned u = __float_as_uint(x);
@@ -905,18 +906,15 @@ __global__ void __launch_bounds__(256) vcopy_kernel(PrefillArgs a) {
     }
 }
 
-// 4-bit pools: the keys are copied too, widened exactly to bf16 in the bf16
-// pools' layout, and the values to fp16 at their step's scale as above.  Wave w
-// takes page w of the step: lane (blk, tok) 32 dims of a key, lane (q, n) dims
-// 16 t + n of slots 4q..4q+3.  A page outside the pool leaves NaN keys.
+// 4-bit pools: the values widened to fp16 at their step's scale as above.  Wave w
+// takes page w of the step, lane (q, n) dims 16 t + n of slots 4q..4q+3.
 template <int D>
-__global__ void __launch_bounds__(256) kv4copy_kernel(PrefillArgs a) {
+__global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
     constexpr int TB = kTile4Rows * D / 2;
     using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
     __shared__ float wmax[2][4];
     const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int blk = D == 128 ? qg : qg & 1;
     const bool self = a.B <= 64;
     int s_end = 0, total, Lb = 0;
     if (self) {
@@ -946,12 +944,7 @@ __global__ void __launch_bounds__(256) kv4copy_kernel(PrefillArgs a) {
         const int nv = max(min(L - kPage * pi, kPage), 0);        // live slots of this wave's page
         const int pg = nv > 0 ? a.block_table[(int64_t)b * a.bt_stride + pi] : 0;
         const bool ok = (unsigned)pg < (unsigned)a.num_pages;
-        if (!ok && lane == 0) atomicOr(a.err, kErrPage);
-        const int64_t tile = ((int64_t)(ok ? pg : 0) * a.H_kv + g) * TB;
-        const char* kp = (const char*)a.k_pages + tile;
-        const char* vp = (const char*)a.v_pages + tile;
-        const u32x4 kc = *(const u32x4*)(kp + blk * 256 + n * 16);
-        const uint32_t ksb = *(const uint8_t*)(kp + 8 * D + blk * 16 + n);
+        const char* vp = (const char*)a.v_pages + ((int64_t)(ok ? pg : 0) * a.H_kv + g) * TB;
         const VT vc = *(const VT*)(vp + lane * (D / 8));
         const VT vs = *(const VT*)(vp + 8 * D + qg * (D / 8));
         float v[D / 16][4];
@@ -975,17 +968,6 @@ __global__ void __launch_bounds__(256) kv4copy_kernel(PrefillArgs a) {
                 }
             }
         }
-        const int64_t page = (t * (kPrefillKeys / kPage) + w) * (int64_t)(D * kPage);
-        if (D == 128 || lane < 32) {
-            // NaN, or 0 past the length
-            const float ks = !ok ? __uint_as_float(0x7fc00000u) : n < nv ? scale_of4(ksb) : 0.f;
-            uint16_t* dst = a.kcopy + page + blk * (4 * kPage * 8) + n * 8;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(u32x4*)(dst + i * (kPage * 8)) =
-                    u32x4{pair4_bf16(pair4<0>(kc[i], ks)), pair4_bf16(pair4<1>(kc[i], ks)),
-                          pair4_bf16(pair4<2>(kc[i], ks)), pair4_bf16(pair4<3>(kc[i], ks))};
-        }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
         if (lane == 0) wmax[par][w] = m;
@@ -994,7 +976,7 @@ __global__ void __launch_bounds__(256) kv4copy_kernel(PrefillArgs a) {
         const int e = vcopy_exp(__float_as_uint(m));
         if (threadIdx.x == 0) a.vexp[t] = e;
         const float sc = e == kAnyExp ? 1.f : pow2f(e);
-        uint16_t* dst = a.vcopy + page + n * kPage + 4 * qg;
+        uint16_t* dst = a.vcopy + (t * (kPrefillKeys / kPage) + w) * (int64_t)(D * kPage) + n * kPage + 4 * qg;
 #pragma unroll
         for (int tt = 0; tt < D / 16; ++tt) {
             const f32x2 lo = {v[tt][0] * sc, v[tt][1] * sc}, hi = {v[tt][2] * sc, v[tt][3] * sc};
@@ -1070,8 +1052,14 @@ constexpr int kValuPerMfma = 7;
 // s ^ 4, so every 8 (and 16) consecutive lanes of a read touch distinct
 // banks.
 //
-// KC (4-bit pools): K tiles too come from a copy, laid out as bf16 pools are.
-template <int D, int NH, bool FP8, bool KC>
+// FP4 (4-bit pools): K tiles reach LDS as they lie, codes and scales, and are A
+// of v_mfma_scale_f32_32x32x64_f8f6f4 as e2m1 (lane (h, i): row i, k = 32 h ..
+// 32 h + 31, its scale), no widening.  B holds the query as e4m3 terms hi + lo,
+// scaled by a power of two a column (lane (h, c): k = 16 h + 0..15 and 32 + 16 h +
+// 0..15), exact for bf16 within 2^-14 of the row's largest: two products of 64
+// dims at twice bf16's rate.  Values come from the fp16 copy.  Eight chats' 16-256
+// new tokens after 2-8k: see launch_prefill_prep.
+template <int D, int NH, bool FP8, bool FP4>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_attn_kernel(PrefillArgs a) {
     constexpr int KS = 32 * NH;         // keys per step
@@ -1082,14 +1070,16 @@ prefill_attn_kernel(PrefillArgs a) {
     constexpr int KT = PPS * PE;        // a step's K (or V) tile, elements
     constexpr int PBP = FP8 ? PB + 128 : PB;   // LDS bytes from one page of a tile to the next
     constexpr int KTW = PPS * PBP / 2;  // the tile in 16-bit words
+    constexpr int C4 = 8 * D, S4 = D / 2;      // FP4: code and scale bytes of a K page
+    constexpr int KW4 = PPS * (C4 + S4) / 2;   // its K tile in LDS: the pages' codes, then their scales
     constexpr int UPP = PB / 16;        // 16-byte units per page
     constexpr int PER = 2 * PPS * UPP / 256;   // units of K + V per thread per step
     constexpr int WIN = kPageWindow / PPS;     // steps per block-table window
-    __shared__ __attribute__((aligned(16))) uint16_t kb0[KTW];
-    __shared__ __attribute__((aligned(16))) uint16_t kb1[KTW];
+    __shared__ __attribute__((aligned(16))) uint16_t kb0[FP4 ? KW4 : KTW];
+    __shared__ __attribute__((aligned(16))) uint16_t kb1[FP4 ? KW4 : KTW];
     __shared__ __attribute__((aligned(16))) uint16_t vb0[KTW];
     __shared__ __attribute__((aligned(16))) uint16_t vb1[KTW];
-    __shared__ int pages[KC ? 1 : kPageWindow];
+    __shared__ int pages[kPageWindow];
     __shared__ int vexps[FP8 ? 1 : WIN];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -1171,8 +1161,43 @@ prefill_attn_kernel(PrefillArgs a) {
         v_scale = a.v_scale[(int64_t)b * a.H_kv + g];
     }
     const float sl = fabsf(s_eff);
-    bf16x8 qv[D / 16];
-    {
+    bf16x8 qv[FP4 ? 1 : D / 16];
+    i32x8 q_hi[FP4 ? D / 64 : 1], q_lo[FP4 ? D / 64 : 1];
+    int qs_hi = 0, qs_lo = 0;
+    if constexpr (FP4) {
+        // scaled so that the row's largest magnitude lies in [2^7, 2^8); the
+        // instruction's scales take that out, and lo's 2^4
+        const uint32_t flip = s_eff < 0.f ? 0x80008000u : 0u;
+        const uint16_t* qrow = a.q + (int64_t)(t0 + tok) * a.q_st + (int64_t)h * a.q_sh + 16 * hl;
+        u32x4 u[D / 16];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            u[i] = *(const u32x4*)(qrow + 32 * (i >> 1) + 8 * (i & 1)) ^ flip;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m = max(m, max(u[i][k] & 0x7fffu, (u[i][k] >> 16) & 0x7fffu));
+        }
+        m = max(m, __float_as_uint(swap_halves(__uint_as_float(m))));
+        const int k = max(-120, min(134 - (int)(m >> 7), 120));
+        const float sq = __uint_as_float((uint32_t)(k + 127) << 23);
+        qs_hi = 127 - k;
+        qs_lo = 123 - k;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {          // four dims a dword
+                const u32x4 w4 = u[4 * j + (i >> 1)];
+                const uint32_t w0 = i & 1 ? w4.z : w4.x, w1 = i & 1 ? w4.w : w4.y;
+                const float v[4] = {__uint_as_float(w0 << 16) * sq, __uint_as_float(w0 & 0xffff0000u) * sq,
+                                    __uint_as_float(w1 << 16) * sq, __uint_as_float(w1 & 0xffff0000u) * sq};
+                int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+                c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+                const f32x2 h01 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+                q_hi[j][i] = c;
+                c = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[0] - h01.x), 16.f * (v[1] - h01.y), 0, false);
+                q_lo[j][i] = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[2] - h23.x), 16.f * (v[3] - h23.y), c, true);
+            }
+    } else {
         const uint32_t flip = s_eff < 0.f ? 0x80008000u : 0u;
         // the B operand of MFMA kb: dims 16 kb + 8 hl (fp8: 32 (kb / 2) + 16 hl + 8 (kb % 2))
         const uint16_t* qrow = a.q + (int64_t)(t0 + tok) * a.q_st + (int64_t)h * a.q_sh + (FP8 ? 16 : 8) * hl;
@@ -1201,14 +1226,14 @@ prefill_attn_kernel(PrefillArgs a) {
 #pragma unroll
         for (int k = 0; k < kPageWindow / 256; ++k) {
             const int e = 256 * k + tid;
-            if (!KC && e >= e0 && e < e1) pe[k] = bt[min(PPS * j + e, np - 1)];
+            if (e >= e0 && e < e1) pe[k] = bt[min(PPS * j + e, np - 1)];
         }
         const bool mine = !FP8 && PPS * tid >= e0 && PPS * tid < e1;
         if (mine) ve = a.vexp[(int64_t)(vstep0 + j + tid) * a.H_kv + g];
 #pragma unroll
         for (int k = 0; k < kPageWindow / 256; ++k) {
             const int e = 256 * k + tid;
-            if (!KC && e >= e0 && e < e1) pages[e] = pe[k];
+            if (e >= e0 && e < e1) pages[e] = pe[k];
         }
         if (mine) vexps[tid] = ve;
         __syncthreads();
@@ -1219,16 +1244,16 @@ prefill_attn_kernel(PrefillArgs a) {
     // step s computes, K of step s + 2 and V of step s + 1 are loaded into
     // registers, and written to LDS after it.
     constexpr int PERH = PER / 2;      // units of one tensor per thread per step
-    const char* kbase = (const char*)a.k_pages + (int64_t)g * PB;
+    const char* kbase = (const char*)a.k_pages + (int64_t)g * (FP4 ? C4 + S4 : PB);
     const char* vbase = (const char*)a.v_pages + (int64_t)g * PB;
-    const int64_t page_bytes = (int64_t)a.H_kv * PB;
+    const int64_t page_bytes = (int64_t)a.H_kv * (FP4 ? C4 + S4 : PB);
     // bf16 pools: the values come from the fp16 copy, whose steps of request b
     // are consecutive from vstep0
     const char* vbase16 = FP8 ? nullptr : (const char*)a.vcopy + ((int64_t)vstep0 * a.H_kv + g) * (PPS * PB);
-    const char* kbase16 = KC ? (const char*)a.kcopy + ((int64_t)vstep0 * a.H_kv + g) * (PPS * PB) : nullptr;
     int64_t off1[PPS], off2[PPS];      // page byte offsets of steps s + 1 and s + 2
+    int bad1 = 0, bad2 = 0;            // FP4: the pages of the steps computed next that lie outside the pool
     auto pages_of = [&](int j, int64_t (&off)[PPS]) {
-        if constexpr (KC) return;
+        int outside = 0;
         const int e = PPS * (j % WIN);
 #pragma unroll
         for (int q = 0; q < PPS; ++q) {
@@ -1236,9 +1261,11 @@ prefill_attn_kernel(PrefillArgs a) {
             if ((unsigned)pg >= (unsigned)a.num_pages) {
                 pg = 0;
                 bad = true;
+                outside |= 1 << q;
             }
             off[q] = (int64_t)pg * page_bytes;
         }
+        return outside;
     };
     // direct copies into LDS: lane l of a wave lands at unit (wave base + l);
     // it fetches the global unit the swizzle maps there (the swizzles are
@@ -1289,18 +1316,25 @@ prefill_attn_kernel(PrefillArgs a) {
                                              0, 0);
         }
     };
-    // the keys of step j: from the pool's pages, or from their copy
-    auto dma_k = [&](int j, const int64_t (&off)[PPS], uint16_t* dst) {
-        if constexpr (!KC) {
+    // the keys of a step.  FP4: unit tid of the step's 16-byte code units (a wave's
+    // 64 lie in one page, or two at head_dim 64), and the last wave the scale
+    // words
+    auto dma_k = [&](const int64_t (&off)[PPS], uint16_t* dst) {
+        if constexpr (!FP4) {
             dma(kbase, off, dst, false);
         } else {
-            const char* src = kbase16 + (int64_t)j * a.H_kv * (PPS * PB);
-#pragma unroll
-            for (int k = 0; k < PERH; ++k) {
-                const int v = ((256 * k + 64 * w) % UPP) + lane;
-                const int vg = v ^ (((v >> 3) & 1) << 2);
-                __builtin_amdgcn_global_load_lds(src + (256 * k + 64 * w - v + lane + vg) * 16,
-                                                 dst + 8 * (256 * k + 64 * w), 16, 0, 0);
+            constexpr int U = C4 / 16, SW = S4 / 4;    // units and scale words of a page
+            // (values, so that the selects are not of addresses, which would put off[] into memory)
+            const int64_t o0 = off[0], o1 = off[1], o2 = off[2], o3 = off[3];
+            if (D == 128 || w < 2) {
+                const int64_t o = D == 128 ? (w & 2 ? (w & 1 ? o3 : o2) : (w & 1 ? o1 : o0))
+                                           : (w & 1 ? (lane < 32 ? o2 : o3) : (lane < 32 ? o0 : o1));
+                __builtin_amdgcn_global_load_lds(kbase + o + (lane % U) * 16, dst + 64 * 8 * w, 16, 0, 0);
+            }
+            if (w == 3 && lane < PPS * SW) {
+                const int p = lane / SW;
+                const int64_t o = p & 2 ? (p & 1 ? o3 : o2) : (p & 1 ? o1 : o0);
+                __builtin_amdgcn_global_load_lds(kbase + o + C4 + (lane % SW) * 4, dst + PPS * C4 / 2, 4, 0, 0);
             }
         }
     };
@@ -1358,10 +1392,33 @@ prefill_attn_kernel(PrefillArgs a) {
         return *(const u32x4*)((const char*)Vt0 + hh * 2 * PBP + (32 * t) * 16 + v_off8);
     };
 
+    // FP4: key kk's 16 code bytes of block hl, and its scale byte
+    const int k_off4 = (kk >> 4) * C4 + hl * 256 + (kk & 15) * 16;
+    const int s_off4 = PPS * C4 + (kk >> 4) * S4 + hl * 16 + (kk & 15);
     auto qk = [&](const uint16_t* Kt, f32x16 (&sc)[NH]) {
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh) sc[hh] = f32x16{};
-        if constexpr (FP8) {
+        if constexpr (FP4) {
+            u32x4 kc[NH][D / 64];
+            int ks[NH][D / 64];
+#pragma unroll
+            for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    kc[hh][j] = *(const u32x4*)((const char*)Kt + hh * 2 * C4 + j * 512 + k_off4);
+                    ks[hh][j] = *((const uint8_t*)Kt + hh * 2 * S4 + j * 32 + s_off4);
+                }
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int hh = 0; hh < NH; ++hh) {
+                        const i32x8 ka = {(int)kc[hh][j].x, (int)kc[hh][j].y, (int)kc[hh][j].z, (int)kc[hh][j].w, 0, 0, 0, 0};
+                        sc[hh] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                            ka, e ? q_lo[j] : q_hi[j], sc[hh], 4 /* e2m1 */, 0 /* e4m3 */, 0, ks[hh][j], 0, e ? qs_lo : qs_hi);
+                    }
+        } else if constexpr (FP8) {
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
                 u32x4 ku[NH];
@@ -1398,9 +1455,9 @@ prefill_attn_kernel(PrefillArgs a) {
     // prologue: K and V of the first step, K of the next, S of the first
     if (s_lo < s_hi) {
         refill(s_lo / WIN * WIN);
-        pages_of(s_lo, off2);
+        bad1 = pages_of(s_lo, off2);
         e1 = vexp_of(s_lo);
-        dma_k(s_lo, off2, kb0);
+        dma_k(off2, kb0);
         if constexpr (FP8) dma(vbase, off2, vb0, true);
         else dma_v16(s_lo, vb0);
         if (s_lo + 1 < s_hi) {
@@ -1408,9 +1465,9 @@ prefill_attn_kernel(PrefillArgs a) {
                 __syncthreads();       // every wave has read the first step's pages
                 refill(s_lo + 1);
             }
-            pages_of(s_lo + 1, off1);
+            bad2 = pages_of(s_lo + 1, off1);
             e2 = vexp_of(s_lo + 1);
-            dma_k(s_lo + 1, off1, kb1);
+            dma_k(off1, kb1);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -1432,16 +1489,16 @@ prefill_attn_kernel(PrefillArgs a) {
         uint16_t* v_rd = P ? vb1 : vb0;   // V(s)
         uint16_t* v_wr = P ? vb0 : vb1;   // V(s + 1), over V(s - 1)
         const bool more_k = s + 2 < s_hi, more_v = s + 1 < s_hi;
-        int e3 = kAnyExp;
+        int e3 = kAnyExp, bad3 = 0;
         if (more_v) {
             if constexpr (FP8) dma(vbase, off1, v_wr, true);
             else dma_v16(s + 1, v_wr);
         }
         if (more_k) {
             if ((s + 2) % WIN == 0) refill(s + 2);
-            pages_of(s + 2, off2);
+            bad3 = pages_of(s + 2, off2);
             e3 = vexp_of(s + 2);
-            dma_k(s + 2, off2, k_wr);
+            dma_k(off2, k_wr);
         }
         // the weights' factor 2^-d of this step, as the exponent's offset, and
         // 2^d, which takes their sum back (d in [-7, 0], above 0 only past
@@ -1465,6 +1522,13 @@ prefill_attn_kernel(PrefillArgs a) {
         }
         uint32_t ph[NH][8];   // P as fp16 pairs
         if (s < wave_steps) {
+            if (FP4 && bad1) {          // keys of a page outside the pool score NaN
+#pragma unroll
+                for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (bad1 >> (2 * hh + (j >> 3)) & 1) sc[hh][j] = __builtin_nanf("");
+            }
             // keys above a column's position are masked only on the steps
             // the wave's diagonal crosses
             if (KS * s + KS - 1 > pos_w) {
@@ -1509,13 +1573,15 @@ prefill_attn_kernel(PrefillArgs a) {
             // VALU work spread between them
             // (fp8: one K read per two MFMAs)
             constexpr int KR = FP8 ? 2 : 1;
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            // FP4: 4 NH products of twice the length, their K reads all ahead
+            constexpr int NM = FP4 ? D / 32 * NH : 8 * NH;
+            __builtin_amdgcn_sched_group_barrier(0x100, FP4 ? D / 32 * NH : 2, 0);
 #pragma unroll
-            for (int i = 0; i < 8 * NH; ++i) {
+            for (int i = 0; i < NM; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);        // an MFMA of S
-                if (i % KR == KR - 1 && i / KR + 2 < 8 * NH / KR)
+                if (!FP4 && i % KR == KR - 1 && i / KR + 2 < 8 * NH / KR)
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // a K read
-                __builtin_amdgcn_sched_group_barrier(0x002, kValuPerMfma, 0);   // softmax VALU
+                __builtin_amdgcn_sched_group_barrier(0x002, FP4 ? 2 * kValuPerMfma : kValuPerMfma, 0);   // softmax VALU
             }
             // O^T += V^T P^T, per 16-key group u of each half and 32-dim tile t
             // (bf16: group u is page u; fp8: keys 8 u .. 8 u + 7 of the
@@ -1572,6 +1638,8 @@ prefill_attn_kernel(PrefillArgs a) {
         for (int q = 0; q < PPS; ++q) off1[q] = off2[q];
         e1 = e2;
         e2 = e3;
+        bad1 = bad2;
+        bad2 = bad3;
     };
     // unrolled by two so that S(s) and S(s + 1) alternate between register sets
     for (int s = s_lo; s < s_hi; s += 2) {
@@ -1743,9 +1811,9 @@ void launch_kv_read(const WriteArgs& a, int32_t* page_start, hipStream_t s) {
 void launch_prefill_prep(const PrefillArgs& a, hipStream_t s) {
     if (a.B > 64) hipLaunchKernelGGL(prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     if (a.fp8) return;
-    if (a.kcopy) {
-        if (a.D == 128) hipLaunchKernelGGL(kv4copy_kernel<128>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(kv4copy_kernel<64>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
+    if (a.fp4) {
+        if (a.D == 128) hipLaunchKernelGGL(v4copy_kernel<128>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(v4copy_kernel<64>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
         return;
     }
     if (a.D == 128) hipLaunchKernelGGL(vcopy_kernel<128>, dim3((unsigned)a.vgrid), dim3(256), 0, s, a);
@@ -1755,7 +1823,7 @@ void launch_prefill_prep(const PrefillArgs& a, hipStream_t s) {
 void launch_prefill_attn(const PrefillArgs& a, hipStream_t s) {
     constexpr int NH = kPrefillKeys / 32;
     const dim3 grid((unsigned)((a.max_units + kXcds - 1) / kXcds * kXcds));
-    if (a.kcopy) {
+    if (a.fp4) {
         if (a.D == 128)
             hipLaunchKernelGGL((prefill_attn_kernel<128, NH, false, true>), grid, dim3(256), 0, s, a);
         else
