@@ -2,7 +2,11 @@
 // attention: y = R(p) (x / sqrt(mean(x^2) + eps) * (w + offset)) per head row,
 // R(p) turning each pair of the first R dims by position times frequency.
 //
-// Bound by memory: (H_q + H_kv) D values a token read and written once.  A row
+// Bound by memory: (H_q + H_kv) D values a token read and written once (36,001
+// tokens of 32/8 heads of 128, 737 MB, in 137-141 us, 5.2-5.4 TB/s; 4,613 of 28/4
+// in 16.1 us; 64 tokens 4.1 us, a launch's latency).  Six waves a SIMD (68
+// registers; at four, 8,000 tokens of 64 dims took 23 us instead of 17.4, and
+// loads a pass ahead cost more registers than they hid).  A row
 // is D / 16 lanes, each with two 16-byte units whose values pair up (dims i and
 // i + R / 2, or neighbours), so nothing crosses lanes but the sum of squares; a
 // wave walks a token's rows, 64 / (D / 16) at a time, queries first.  A lane's
@@ -54,7 +58,7 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 
 template <int D, bool INTER>
-__global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a) {
+__global__ void __launch_bounds__(256, 6) qk_norm_rope_kernel(RopeArgs a) {
     constexpr int LPR = D / 16, RPW = 64 / LPR;     // lanes a row, rows a pass
     const int lane = threadIdx.x & 63, j = lane % LPR, sub = lane / LPR;
     const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -153,9 +157,10 @@ void launch_qk_norm_rope(const RopeArgs& args, hipStream_t s) {
     RopeArgs a = args;
     const int rpw = 64 / (a.D / 16);
     const int passes = (a.H_q + rpw - 1) / rpw + (a.H_kv + rpw - 1) / rpw;
-    // A token's passes go over as many waves as it takes to have 8192 (eight a
-    // SIMD); from 8192 tokens on one wave takes a token and forms its angles once.
-    a.chunks = (int)std::min<int64_t>(passes, (8192 + a.T - 1) / a.T);
+    // A token's passes go over as many waves as it takes to have 4096 (four a
+    // SIMD); from 4096 tokens on one wave takes a token and forms its angles once
+    // (2048 tokens of 32/8 heads of 128: 11.9 us at 4096, 12.8 at 8192).
+    a.chunks = (int)std::min<int64_t>(passes, (4096 + a.T - 1) / a.T);
     const dim3 grid((unsigned)(((int64_t)a.T * a.chunks + 3) / 4));
     if (a.D == 128) {
         if (a.interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), grid, dim3(256), 0, s, a);
