@@ -437,17 +437,18 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     // 0.5-8k, 77 table pages a wave, 26.9 / 26.2, 28 of them, 108 pages, 31.2 /
     // 31.4 at 4 heads and 34.6 / 32.4 at 8).
     // Over 4-bit pools a step is half an fp8 step's bytes and as many
-    // instructions: at head_dim 64 the second workgroup pays from short shares on
-    // (300 requests of 2-8k 182 / 229 us, 64 of 1-4k 29.5 / 33.8, 20 of 0.5-8k, 78
-    // table pages a wave, 23.7 / 22.4); at head_dim 128 one reads the pages as
-    // fast as two until the shares are long (256 of 6-13.5k 470 / 466 us on one
-    // device, 480 / 492 on another, 512 with Zipf lengths to 8k 194 / 197, 400 of
-    // 3-5k 317 / 318, 64 of 1-4k 43 / 42, 16 heads, 256 of 6-13.5k, 81 / 75).
+    // instructions, and the second workgroup pays from shorter shares on (two /
+    // one, table pages a wave of one in brackets): at head_dim 128 and 4 heads, 256
+    // requests of 6-13.5k [1690] 448 / 474 us, 400 of 3-5k [980] 299 / 308, 100 of
+    // 4-8k [390] 116.7 / 121.1, 128 of 2-6k [375] 104.5 / 103.7, 64 of 1-4k [128]
+    // 42.6 / 41.6, at 16 heads 256 of 6-13.5k on one KV head 81.5 / 77.9; at
+    // head_dim 64, 300 of 2-8k [1170] 175 / 230, 64 of 1-4k [128] 28.4 / 33.4, 40
+    // of them [80] 23.6 / 24.1, 20 of 0.5-8k [78] 25.5 / 22.8.
     bool two = chosen && ps.fp8 &&
                (ps.D == 64 ? table_pages_per_wave >= std::max(96.0, 14.0 * (double)G)
                            : G <= 8 && table_pages_per_wave >= kWideTablePages);
     if (chosen && ps.fp4)
-        two = ps.D == 64 ? table_pages_per_wave >= 96.0 : G <= 8 && table_pages_per_wave >= 1280.0;
+        two = ps.D == 64 ? table_pages_per_wave >= 96.0 : G <= 8 && table_pages_per_wave >= 384.0;
     const int wgs = chosen && !two ? 1 : bpc;
     const int64_t cu_waves = (int64_t)g_cu_count[dev] * (kAttnBlock / kWaveSize);
     int64_t waves = cu_waves * wgs, sized = cu_waves * (depth == asked_depth ? bpc : 1);
@@ -505,6 +506,8 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     a.max_pages = (int)max_pages;
     a.waves = (int)waves;
     a.pp = pps;
+    a.hs = 1;
+    while (ps.fp4 && a.hs < kAttnBlock / kWaveSize && ps.H_kv % (2 * a.hs) == 0 && waves % (2 * a.hs) == 0) a.hs *= 2;
     // The default XCD weights were measured on a whole MI355X (256 CUs,
     // workgroup i on XCD i mod 8), with one and with two workgroups per CU;
     // partitioned devices keep equal shares.

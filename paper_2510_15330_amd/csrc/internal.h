@@ -69,6 +69,7 @@ struct AttnArgs {
     int B, H_q, H_kv, G, D, max_pages;
     int waves;           // waves sharing the flattened step stream (the grid's waves)
     int pp;              // pages per step of the launched attention kernel
+    int hs;              // 4-bit pools: heads that neighbouring waves take side by side (divides waves and H_kv)
     int skew;            // share weights 256 + skew (even-XCD workgroups) / 256 - skew on long shares; 0..255
                          // (work_split.h)
     int32_t* err;        // the device's error word

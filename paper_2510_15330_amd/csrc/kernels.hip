@@ -1062,9 +1062,10 @@ __device__ __forceinline__ void cursor_len(Cursor& c) {
 }
 
 // Step to the next unit.  A cursor that would leave the range keeps its last
-// position (so loads issued for it stay in bounds) and stops being live.
+// position (so loads issued for it stay in bounds) and stops being live.  The
+// wave's heads are g0, g0 + hs, ...
 template <int PP, bool STEP>
-__device__ __forceinline__ void cursor_next(Cursor& c, const AttnArgs& a, int r1) {
+__device__ __forceinline__ void cursor_next(Cursor& c, const AttnArgs& a, int r1, int hs, int g0) {
     if (!c.live) return;
     if (c.x + 1 >= r1) {
         c.live = false;
@@ -1074,8 +1075,9 @@ __device__ __forceinline__ void cursor_next(Cursor& c, const AttnArgs& a, int r1
     c.p += PP;
     if (c.p >= c.np) {
         c.p = 0;
-        if (++c.g >= a.H_kv) {
-            c.g = 0;
+        c.g += hs;
+        if (c.g >= a.H_kv) {
+            c.g = g0;
             // units remain, so a later request with pages exists
             do {
                 ++c.b;
@@ -1116,6 +1118,18 @@ attn_mfma_kernel(AttnArgs a) {
     // wave index, made provably uniform so that all stream bookkeeping is scalar
     const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kAttnBlock / kWaveSize) + (threadIdx.x >> 6));
     if (w >= a.waves) return;
+    // 4-bit pools: hs neighbouring waves of a workgroup (4, 2 or 1) take the same
+    // share of the (request, group of hs heads, step) units, a head each.  A
+    // tile's ends lie inside cache lines that hold its neighbours' too (8.5
+    // lines a tile at head_dim 128, 4.25 at 64), which are then in flight
+    // together (256 requests of 6-13.5k tokens 477 -> 470 us, 512 with Zipf
+    // lengths to 8k 194 -> 187; with the scales' loads not streamed 457 and
+    // 184, all loads not streamed 504 and 195).  Wave v of the plan, and of the pieces: the waves of
+    // one head of the groups, one after the other.
+    const int hs = FP4 ? a.hs : 1;
+    const int wg = FP4 ? w / hs : w;
+    const int g0 = FP4 ? w % hs : 0;
+    const int v = FP4 ? g0 * (a.waves / hs) + wg : w;
     uint64_t t_start = 0;
     if constexpr (TRACE) t_start = __builtin_amdgcn_s_memrealtime();
     auto trace_end = [&]() {
@@ -1154,7 +1168,7 @@ attn_mfma_kernel(AttnArgs a) {
             const bool in = b0 + kWaveSize * k + lane < a.B;
             if (in && (Lk[k] < 0 || Lk[k] > maxL)) bad_len = true;
             Lk[k] = in ? attn_len<STEP>(a, Lk[k]) : 0;
-            uk[k] = ((Lk[k] + kPage - 1) / kPage + PP - 1) / PP * a.H_kv;
+            uk[k] = ((Lk[k] + kPage - 1) / kPage + PP - 1) / PP * (FP4 ? a.H_kv / hs : a.H_kv);
             sum += uk[k];
         }
         return sum;
@@ -1188,16 +1202,16 @@ attn_mfma_kernel(AttnArgs a) {
         zero_empty(b0);
     }
     const int P = __builtin_amdgcn_readlane(lane_scan(lsum), kWaveSize - 1);
-    const int W = min(a.waves, P);     // no more waves than units take a share
-    const int skew = share_skew(a.skew, P, W, PP);
+    const int W = min(a.waves, P * hs);     // no more waves than units take a share
+    const int skew = share_skew(a.skew, P * hs, W, PP);
     // wave 0 raises the length flag
     if (w == 0 && __any(bad_len) && lane == 0) atomicOr(a.err, kErrLength);
-    const int r0 = w < W ? share_bound(w, P, W, skew) : 0;
-    const int r1 = w < W ? share_bound(w + 1, P, W, skew) : 0;
+    const int r0 = w < W ? share_bound(wg * hs, P, W, skew) : 0;
+    const int r1 = w < W ? share_bound((wg + 1) * hs, P, W, skew) : 0;
     if (r0 >= r1) {
-        if (lane == 0) a.cuts[w] = make_int4(-1, 0, 0, 0);
+        if (lane == 0) a.cuts[v] = make_int4(-1, 0, 0, 0);
         // a share that an extreme weight leaves empty: its piece is dead
-        if (w < W && lane < a.G) a.part_ml[2 * (int64_t)w * a.G + lane] = make_float2(-INFINITY, 0.f);
+        if (w < W && lane < a.G) a.part_ml[2 * (int64_t)v * a.G + lane] = make_float2(-INFINITY, 0.f);
         trace_end();
         return;
     }
@@ -1220,6 +1234,7 @@ attn_mfma_kernel(AttnArgs a) {
                 const int ns = ((sL + kPage - 1) / kPage + PP - 1) / PP;
                 sg = (int)((unsigned)off / (unsigned)ns);
                 sp = (off - sg * ns) * PP;
+                sg = sg * hs + g0;
             }
             carry = __builtin_amdgcn_readlane(incl, kWaveSize - 1);
         }
@@ -1308,7 +1323,7 @@ attn_mfma_kernel(AttnArgs a) {
 #pragma unroll
     for (int j = 1; j < DEPTH + 2; ++j) {
         cur[j] = cur[j - 1];
-        cursor_next<PP, STEP>(cur[j], a, r1);
+        cursor_next<PP, STEP>(cur[j], a, r1, hs, g0);
     }
 
     // Block-table entries of a step: lane i < PP reads page p + i, clamped to
@@ -1405,8 +1420,9 @@ attn_mfma_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) r.v[i] = ld_stream_at<typename P4::VT>(vb[i], v_off);
         const size_t s_off = own + 8 * D + 4 * P4::scale_word(lane);
-        r.ks = ld_stream<uint32_t>((const char*)a.k_pages + s_off);
-        r.vs = ld_stream<uint32_t>((const char*)a.v_pages + s_off);
+        // (not streamed: the line stays for the neighbouring tile that shares it)
+        r.ks = *(const uint32_t*)((const char*)a.k_pages + s_off);
+        r.vs = *(const uint32_t*)((const char*)a.v_pages + s_off);
     };
 
     // m starts at the lowest finite value: scores of -inf alone weigh nothing
@@ -1446,7 +1462,7 @@ attn_mfma_kernel(AttnArgs a) {
                     *(u32x2*)(orow + 16 * t + 4 * qg) = pk;
                 }
             } else {
-                const int64_t slot = (int64_t)(2 * w + kind) * a.G + n;
+                const int64_t slot = (int64_t)(2 * v + kind) * a.G + n;
                 float* po = a.part_o + slot * D;
                 const float f = seg_bad ? NAN : vs;
 #pragma unroll
@@ -1544,7 +1560,7 @@ attn_mfma_kernel(AttnArgs a) {
         if (C.live && (C.p + C.len >= C.np || C.x + 1 >= r1)) finish(C, vs);
 #pragma unroll
         for (int j = 0; j < DEPTH + 1; ++j) cur[j] = cur[j + 1];
-        cursor_next<PP, STEP>(cur[DEPTH + 1], a, r1);
+        cursor_next<PP, STEP>(cur[DEPTH + 1], a, r1, hs, g0);
     };
 
     // One exit, after a whole round of DEPTH + 1 steps.  An exit between
@@ -1582,8 +1598,9 @@ attn_mfma_kernel(AttnArgs a) {
     const int en = (e.np + PP - 1) / PP;
     if (lane == 0) {
         const bool cut = ex0 >= r0 && ex0 + en > r1;
-        const int wl = cut ? wave_of(ex0 + en - 1, P, W, skew) : 0;
-        a.cuts[w] = cut ? make_int4(e.b, e.g, wl, 0) : make_int4(-1, 0, 0, 0);
+        int wl = cut ? wave_of(ex0 + en - 1, P, W, skew) : 0;
+        if constexpr (FP4) wl = g0 * (a.waves / hs) + wl / hs;
+        a.cuts[v] = cut ? make_int4(e.b, e.g, wl, 0) : make_int4(-1, 0, 0, 0);
     }
     trace_end();
 }
