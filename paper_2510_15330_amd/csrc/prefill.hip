@@ -414,26 +414,34 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(AppendArgs a) {
     constexpr int TB = kTile4Rows * D / 2;
     constexpr int E = D / 16;             // dims a lane
     const int b = blockIdx.x, lane = threadIdx.x & 63, n = lane & 15;
-    const int w = threadIdx.x >> 6;
-    const int L = a.seq_lens[b];
-    const int pi = L >> 4;
-    const bool in_table = L >= 0 && pi < a.max_pages;
-    const int pg = in_table ? a.block_table[(int64_t)b * a.bt_stride + pi] : -1;
-    const bool ok = pg >= 0 && (int64_t)pg < a.num_pages;
-    if (!ok && threadIdx.x == 0) atomicOr(a.err, kErrAppendSlot);
-    if (!ok) return;
-    const int slot = L & (kPage - 1), q = slot >> 2, r = slot & 3;
-    for (int g = (w >> 1) * 4 + (lane >> 4); g < a.H_kv; g += 8) {
-        if ((w & 1) == 0) {
-            const uint16_t* kn = (const uint16_t*)a.k_new + (int64_t)b * a.new_sb + (int64_t)g * a.new_sh + E * n;
-            char* kp = (char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
-            uint32_t in[E / 2];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // a wave's first rows are out before the length and the page are known
+    int L = 0, pg = -1;
+    auto locate = [&]() {
+        L = a.seq_lens[b];
+        const int pi = L >> 4;
+        const bool in_table = L >= 0 && pi < a.max_pages;
+        pg = in_table ? a.block_table[(int64_t)b * a.bt_stride + pi] : -1;
+        return pg >= 0 && (int64_t)pg < a.num_pages;
+    };
+    bool ok;
+    int g = (w >> 1) * 4 + (lane >> 4);
+    if ((w & 1) == 0) {
+        auto load = [&](int h, uint32_t (&in)[E / 2]) {      // dims E n .. E n + E - 1
+            const uint16_t* kn = (const uint16_t*)a.k_new + (int64_t)b * a.new_sb + (int64_t)min(h, a.H_kv - 1) * a.new_sh + E * n;
 #pragma unroll
             for (int i = 0; i < E / 2; i += 2) {
                 const u32x2 x = *(const u32x2*)(kn + 2 * i);
                 in[i] = x.x;
                 in[i + 1] = x.y;
             }
+        };
+        uint32_t in[E / 2];
+        load(g, in);
+        ok = locate();
+        const int slot = L & (kPage - 1);
+        for (; ok && g < a.H_kv; g += 8) {
+            char* kp = (char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) m = max(m, max(in[i] & 0x7fffu, (in[i] >> 16) & 0x7fffu));
@@ -450,15 +458,23 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(AppendArgs a) {
             if constexpr (D == 128) *(uint32_t*)dst = c;
             else *(uint16_t*)dst = (uint16_t)c;
             if (at == 0) *(uint8_t*)(kp + 8 * D + blk * 16 + slot) = (uint8_t)s;
-        } else {
-            const uint16_t* vn = (const uint16_t*)a.v_new + (int64_t)b * a.vnew_sb + (int64_t)g * a.vnew_sh + n;
+            if (g + 8 < a.H_kv) load(g + 8, in);
+        }
+    } else {
+        auto load = [&](int h, uint32_t (&in)[E]) {          // dims 16 t + n
+            const uint16_t* vn = (const uint16_t*)a.v_new + (int64_t)b * a.vnew_sb + (int64_t)min(h, a.H_kv - 1) * a.vnew_sh + n;
+#pragma unroll
+            for (int t = 0; t < E; ++t) in[t] = vn[16 * t];
+        };
+        uint32_t in[E];
+        load(g, in);
+        ok = locate();
+        const int q = (L & (kPage - 1)) >> 2, r = L & 3;
+        for (; ok && g < a.H_kv; g += 8) {
             char* vp = (char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * TB;
             using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
             VT* dst = (VT*)(vp + (q * 16 + n) * (D / 8));
             VT x = *dst;
-            uint32_t in[E];
-#pragma unroll
-            for (int t = 0; t < E; ++t) in[t] = vn[16 * t];
 #pragma unroll
             for (int blk = 0; blk < D / 32; ++blk) {
                 const uint32_t s = scale4(row_max(max(in[2 * blk] & 0x7fffu, in[2 * blk + 1] & 0x7fffu)));
@@ -467,7 +483,12 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(AppendArgs a) {
                 if (n == blk) *(uint8_t*)(vp + 8 * D + q * (D / 8) + 4 * blk + r) = (uint8_t)s;
             }
             *dst = x;
+            if (g + 8 < a.H_kv) load(g + 8, in);
         }
+    }
+    if (!ok) {
+        if (threadIdx.x == 0) atomicOr(a.err, kErrAppendSlot);
+        return;
     }
     __syncthreads();  // every thread has read seq_lens[b]
     if (threadIdx.x == 0) a.seq_lens[b] = L + 1;
