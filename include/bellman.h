@@ -316,7 +316,9 @@ int bellman_decode_step(const bellman_tensor_t *k_new, const bellman_tensor_t *v
  *   k_pages, v_pages, block_table: as for bellman_kv_append; the pages of
  *                 every new position must already be assigned.
  *   seq_lens      int32 [B] contiguous (read, then advanced).
- * Byte-exact copies (or that quantisation); no other slot changes.  A token outside its
+ * Byte-exact copies (or that quantisation); no other slot changes.  Over 4-bit
+ * pools no two requests of one call may write into the same page (a byte of V
+ * holds two slots).  A token outside its
  * request's table or the pool is skipped and flagged (flag 1), and that
  * request's length is left unchanged when its last position does not fit.
  * Once the workspace has grown to the call's size, the call enqueues only
@@ -331,13 +333,15 @@ int bellman_kv_write(const bellman_tensor_t *k_new, const bellman_tensor_t *v_ne
  * follows the write; whole requests when n_b = L_b), for sharing, moving or
  * checking cached requests.
  *   k_out, v_out  bf16 [T, H_kv, D] (written), innermost contiguous, rows
- *                 16-byte aligned; row q_start[b] + i is token L_b - n_b + i.
+ *                 16-byte aligned, T = q_start[B]; row q_start[b] + i is token
+ *                 L_b - n_b + i.
  * bf16 pools: copies.  fp8 pools (dequant_scale required): code * scale in
  * binary32, rounded to nearest even.  4-bit pools: the exact values (all bf16
  * numbers; beyond bf16's range infinite).  A token whose page lies outside the
  * pool reads as NaN (flag 4); rows of a malformed request (n_b < 0, n_b > L_b,
  * rows past T, L_b past the table) are not written (flag 2), and a q_start
- * that decreases, starts below 0 or ends past T reads no row at all.  Workspace
+ * that decreases, starts below 0 or ends past T reads no row at all, and rows
+ * from q_start[B] on are left as they are (flag 2 in each case).  Workspace
  * and graph capture as for bellman_kv_write. */
 int bellman_kv_read(const bellman_tensor_t *k_pages, const bellman_tensor_t *v_pages,
                     const bellman_tensor_t *block_table, const bellman_tensor_t *seq_lens,

@@ -290,8 +290,8 @@ def test_decode_shapes_and_splits(H_q, H, D, lens):
     c = Cache(rng, lens, H, D).to_device()
     qf, q = bf16(rng.standard_normal((len(lens), H_q, D)) * 2)
     ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * len(lens), D ** -0.5)
-    for kw in ({}, dict(max_waves=1), dict(max_waves=3), dict(max_waves=37), dict(pages_per_step=4),
-               dict(max_waves=6, pages_per_step=4)):
+    for kw in ({}, dict(max_waves=1), dict(max_waves=2), dict(max_waves=3), dict(max_waves=4), dict(max_waves=37),
+               dict(max_waves=40), dict(pages_per_step=4), dict(max_waves=6, xcd_skew=255)):
         out = decode(c, q, D ** -0.5, **kw)
         close(out, ref, mag, dot, DECODE, f"{kw}")
         assert torch.equal(out, decode(c, q, D ** -0.5, **kw)), "not the same twice"
@@ -411,6 +411,57 @@ def test_queries_of_very_different_sizes():
         assert torch.equal(out[:, :8], neg[:, :8])
     # the last row's scores overflow binary32 to both infinities
     assert torch.isnan(out[:, 8]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_that_are_not_finite(D):
+    rng = np.random.default_rng(D)
+    c = Cache(rng, [50, 20], 2, D).to_device()
+    qf, q = bf16(rng.standard_normal((2, 8, D)))
+    q[0, 1, 7] = float("nan")
+    q[0, 6, 0] = float("inf")
+    q[1, 3, D - 1] = -float("inf")
+    bad = torch.zeros((2, 8), dtype=torch.bool, device="cuda")
+    bad[0, 1] = bad[0, 6] = bad[1, 3] = True
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 0.1)
+    pre = torch.empty_like(q)
+    bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.arange(3, dtype=np.int32)), 0.1, pre)
+    for out, tol in ((decode(c, q, 0.1), DECODE), (pre, PROMPT)):
+        assert torch.equal(torch.isnan(out).all(-1), bad) and torch.equal(torch.isnan(out).any(-1), bad)
+        m = ~bad.cpu().numpy()
+        close(out[~bad], ref[m], mag[m], dot[m], tol)
+
+
+def test_pools_beyond_four_gigabytes():
+    """Pages at the far end of pools of 4.5 GiB: every operator's results and
+    bytes are those of the same pages in small pools."""
+    H, D, NP = 8, 128, 556_000
+    rng = np.random.default_rng(77)
+    small = Cache(rng, [60, 33], H, D, room=40).to_device()
+    n = small.pools[0].shape[0]
+    big = [torch.zeros((NP, H, 17, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    assert big[0].numel() > 1 << 32
+    for b, s in zip(big, (small.k, small.v)):
+        b[NP - n:] = s.view(torch.uint8)
+    bt = torch.where(small.bt >= 0, small.bt + (NP - n), small.bt)
+    k, v = torch.randn((42, H, D), device="cuda").to(torch.bfloat16), torch.randn((42, H, D), device="cuda").to(torch.bfloat16)
+    q = torch.randn((42, 4 * H, D), device="cuda").to(torch.bfloat16)
+    got = []
+    for kp, vp, table in ((small.k, small.v, small.bt), (big[0].view(F4), big[1].view(F4), bt)):
+        sl, r = dev(small.lens), []
+        bl.kv_append(k[:2], v[:2], kp, vp, table, sl)
+        out = torch.empty_like(q[:2])
+        bl.decode_attention(q[:2], kp, vp, table, sl, 0.09, out)
+        qs = torch.tensor([0, 30, 40], dtype=torch.int32, device="cuda")
+        bl.kv_write(k[2:], v[2:], kp, vp, table, sl, qs)
+        pre, ko, vo = torch.empty_like(q[2:]), torch.empty_like(k[2:]), torch.empty_like(k[2:])
+        bl.prefill_attention(q[2:], kp, vp, table, sl, qs, 0.09, pre)
+        bl.kv_read(kp, vp, table, sl, qs, ko, vo)
+        got.append([out, pre, ko, vo, sl])
+    assert bl.device_errors() == 0
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and not torch.isnan(got[0][0]).any()
+    for b, s in zip(big, (small.k, small.v)):
+        assert torch.equal(b[NP - n:], s.view(torch.uint8)) and not b[:NP - n].any()
 
 
 def test_bad_pages_and_lengths():

@@ -161,6 +161,10 @@ REFUSED = [
     (["read"], "unaligned rows", dict(vt=t(B.BF16, [20, 8, 128], data=FAKE + 8)), ERR_UNSUPPORTED, "v_out"),
     (["read", "write"], "q_start", dict(qs=t(B.INT32, [4])), ERR_INVALID, "q_start"),
     (["decode", "step"], "one page a step", dict(opts=opts(pages_per_step=1)), ERR_UNSUPPORTED, "pages_per_step"),
+    (["decode", "step"], "eight pages a step", dict(opts=opts(pages_per_step=8)), ERR_UNSUPPORTED, "pages_per_step"),
+    (["decode", "step"], "two steps ahead", dict(opts=opts(pipeline_depth=2)), ERR_UNSUPPORTED, "pipeline_depth"),
+    (EVERY, "too many heads", dict(k=t(B.FP4_E2M1, [1, 70000, 17, 64]), v=t(B.FP4_E2M1, [1, 70000, 17, 64])),
+     ERR_UNSUPPORTED, "65535"),
     (["decode", "step"], "queries of 4 bits", dict(q=t(B.FP4_E2M1, [4, 32, 128])), ERR_INVALID, "q: dtype"),
     (["decode", "step"], "group of 32", dict(q=t(B.BF16, [4, 256, 128]), out=t(B.BF16, [4, 256, 128])), ERR_UNSUPPORTED,
      "group"),
