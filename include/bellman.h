@@ -61,7 +61,8 @@
  *  kept within 2^-127 .. 2^125; each value over the scale is rounded to the
  *  nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even code, 6 at most,
  *  its sign kept.  A block with an infinity or a NaN gets scale 255 and codes
- *  0: it reads as NaN.
+ *  0: it reads as NaN.  No call writes the scales 253 and 254 (values up to
+ *  6 * 2^127): bellman_kv_read takes them, attention over them may overflow.
  */
 #ifndef BELLMAN_H
 #define BELLMAN_H
@@ -368,7 +369,8 @@ int bellman_kv_read(const bellman_tensor_t *k_pages, const bellman_tensor_t *v_p
  *   inv_freq      fp32 [F], contiguous, F a multiple of 8.
  *   q_out, k_out  bf16, shaped as q and k (written, rounded to nearest even):
  *                 q and k themselves, or memory that overlaps no input.
- * Angles are formed in binary64, everything else in binary32.  Enqueues one
+ * Angles are formed in binary64, everything else in binary32 (a normed row whose
+ * squares sum past its range gives zeros).  T below 2^26.  Enqueues one
  * kernel, needs no workspace (graph-capturable).  opts NULL: eps 1e-6, no
  * offset, one axis, pairs (f, f + F). */
 typedef struct bellman_rope_opts {
@@ -419,7 +421,9 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * V scale into the final normalisation.  Over 4-bit pools the keys enter the
  * matrix cores as they lie, against the query as two e4m3 terms (scores as in the
  * decode attention), and the values are copied to fp16 as over
- * bf16 pools; a page outside the pool makes the rows that see it NaN.  Scratch
+ * bf16 pools; a page outside the pool makes the rows that see it NaN, a NaN
+ * key block the (request, head)'s rows that see its token, a NaN value block
+ * its 32 dims of them.  Scratch
  * in the per-device
  * workspace: 3 KiB + 4 (B + 1) bytes; over bf16 and 4-bit pools, for the
  * value copy and its bookkeeping, B ceil(maxP / 4) (4 + 4 H_kv + 128 D H_kv) +

@@ -117,8 +117,11 @@ def attention(q, k_pool, v_pool, table, lens, new, scale):
             s = np.where(np.arange(L)[None, :] > (L - n + np.arange(n))[:, None], -np.inf, s)
             w = np.exp(s - s.max(-1, keepdims=True))
             w /= w.sum(-1, keepdims=True)
-            out[i:i + n, h] = w @ v[:, g]
-            mag[i:i + n, h] = w @ np.abs(v[:, g])
-            dot[i:i + n, h, 0] = (np.abs(q[i:i + n, h]) @ np.abs(k[:, g]).T).max(-1) * abs(scale)
+            seen = np.arange(L)[None, :] <= (L - n + np.arange(n))[:, None]
+            nan = (seen @ np.isnan(v[:, g])) > 0            # of a token that the row sees
+            x = np.nan_to_num(v[:, g])
+            out[i:i + n, h] = np.where(nan, np.nan, w @ x)
+            mag[i:i + n, h] = np.where(nan, np.nan, w @ np.abs(x))
+            dot[i:i + n, h, 0] = np.where(seen, np.abs(q[i:i + n, h]) @ np.abs(k[:, g]).T, 0).max(-1) * abs(scale)
         i += n
     return out, mag, dot

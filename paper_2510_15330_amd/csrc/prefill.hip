@@ -847,6 +847,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(PrefillArgs 
 // the attention holds its output at the finest step's scale and works what a
 // coarser step's is below that into its weights.
 constexpr int kAnyExp = 1 << 20;   // the step's values are all zero: any scale holds
+constexpr int kNanStep = 1 << 21;  // added where a value block of the step is NaN (4-bit pools)
 
 // the scale exponent e for a largest magnitude whose float bits are mb
 // (e = 0 when the maximum is not finite)
@@ -941,12 +942,15 @@ __global__ void __launch_bounds__(256) vcopy_kernel(PrefillArgs a) {
 }
 
 // 4-bit pools: the values widened to fp16 at their step's scale as above.  Wave w
-// takes page w of the step, lane (q, n) dims 16 t + n of slots 4q..4q+3.
+// takes page w of the step, lane (q, n) dims 16 t + n of slots 4q..4q+3.  A NaN
+// block is copied as zeros and the step marked: the attention gives its NaN to
+// the rows that see the token, not to earlier ones of the same step.
 template <int D>
 __global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
     constexpr int TB = kTile4Rows * D / 2;
     using VT = typename std::conditional<D == 128, u32x4, u32x2>::type;
     __shared__ float wmax[2][4];
+    __shared__ int wnan[2][4];
     const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool self = a.B <= 64;
@@ -983,11 +987,16 @@ __global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
         const VT vs = *(const VT*)(vp + 8 * D + qg * (D / 8));
         float v[D / 16][4];
         float m = 0.f;
+        bool has_nan = false;
 #pragma unroll
         for (int bb = 0; bb < D / 32; ++bb) {
             float sc[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sc[r] = scale_of4((vs[bb] >> (8 * r)) & 255u);
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t s = (vs[bb] >> (8 * r)) & 255u;
+                has_nan |= s == kNan4 && 4 * qg + r < nv;
+                sc[r] = s == kNan4 ? 0.f : scale_of4(s);
+            }
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
                 const f32x2 v01 = tt ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vc[bb], 1.0f, 2)
@@ -1004,11 +1013,16 @@ __global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
         }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        if (lane == 0) wmax[par][w] = m;
+        const bool wave_nan = __any(has_nan);
+        if (lane == 0) {
+            wmax[par][w] = m;
+            wnan[par][w] = wave_nan;
+        }
         __syncthreads();            // two sets in turn: the next step's writes cannot pass this step's reads
         m = fmaxf(fmaxf(wmax[par][0], wmax[par][1]), fmaxf(wmax[par][2], wmax[par][3]));
         const int e = vcopy_exp(__float_as_uint(m));
-        if (threadIdx.x == 0) a.vexp[t] = e;
+        if (threadIdx.x == 0)
+            a.vexp[t] = e + (wnan[par][0] | wnan[par][1] | wnan[par][2] | wnan[par][3] ? kNanStep : 0);
         const float sc = e == kAnyExp ? 1.f : pow2f(e);
         uint16_t* dst = a.vcopy + (t * (kPrefillKeys / kPage) + w) * (int64_t)(D * kPage) + n * kPage + 4 * qg;
 #pragma unroll
@@ -1091,8 +1105,9 @@ constexpr int kValuPerMfma = 7;
 // 32 h + 31, its scale), no widening.  B holds the query as e4m3 terms hi + lo,
 // scaled by a power of two a column (lane (h, c): k = 16 h + 0..15 and 32 + 16 h +
 // 0..15), exact for bf16 within 2^-14 of the row's largest: two products of 64
-// dims at twice bf16's rate.  Values come from the fp16 copy.  Eight chats' 16-256
-// new tokens after 2-8k: see launch_prefill_prep.
+// dims at twice bf16's rate.  Values come from the fp16 copy.  Widening the keys
+// to bf16 in LDS instead: eight chats' 16-256 new tokens after 2-8k 122 us, not
+// 112, four 2,048-token chunks after 4-10k 1049, not 996-1019 (whole calls).
 template <int D, int NH, bool FP8, bool FP4>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_attn_kernel(PrefillArgs a) {
@@ -1285,6 +1300,7 @@ prefill_attn_kernel(PrefillArgs a) {
     // are consecutive from vstep0
     const char* vbase16 = FP8 ? nullptr : (const char*)a.vcopy + ((int64_t)vstep0 * a.H_kv + g) * (PPS * PB);
     int64_t off1[PPS], off2[PPS];      // page byte offsets of steps s + 1 and s + 2
+    bool v_nan = false;                // FP4: a step has a NaN value block
     int bad1 = 0, bad2 = 0;            // FP4: the pages of the steps computed next that lie outside the pool
     auto pages_of = [&](int j, int64_t (&off)[PPS]) {
         int outside = 0;
@@ -1538,6 +1554,10 @@ prefill_attn_kernel(PrefillArgs a) {
         // 2^d, which takes their sum back (d in [-7, 0], above 0 only past
         // kMaxRise)
         float d = 0.f, pd = 1.f;
+        if (FP4 && e1 > kAnyExp) {
+            e1 -= kNanStep;
+            v_nan = true;
+        }
         if constexpr (!FP8) {
             if (e1 != kAnyExp) {
                 elow = min(elow, e1);
@@ -1682,6 +1702,25 @@ prefill_attn_kernel(PrefillArgs a) {
     }
     if (bad && lane == 0) atomicOr(a.err, kErrPage);
     if (rw >= rows) return;
+    if (FP4 && v_nan) {
+        // NaN value blocks (copied as zeros) into the rows that see their tokens;
+        // tile t of O is block t.  Lane: a key of the step.
+        for (int s = s_lo; s < min(s_hi, wave_steps); ++s) {
+            const int key = KS * s + lane;
+            int pg = -1;
+            if (key < L) pg = a.block_table[(int64_t)b * a.bt_stride + key / kPage];
+            const bool in = (unsigned)pg < (unsigned)a.num_pages;
+            const char* sc = (const char*)a.v_pages + ((int64_t)(in ? pg : 0) * a.H_kv + g) * (C4 + S4) + C4 +
+                             (key % kPage) / 4 * (D / 8) + key % 4;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) {
+                const uint64_t nans = __ballot(in && *(const uint8_t*)(sc + 4 * t) == kNan4);
+                if (nans != 0u && pos >= KS * s + __ffsll((unsigned long long)nans) - 1)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[t][j] = __builtin_nanf("");
+            }
+        }
+    }
     const float l_tot = l + swap_halves(l);
     // fp8: the V scale; bf16: undo the values' scale, in a multiplication of
     // its own (2^-eref / l may be subnormal where the output is not)

@@ -546,6 +546,37 @@ def test_prompt_page_outside_the_pool():
     assert torch.isnan(out[32:64]).all() and not torch.isnan(out[:32]).any()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_nan_blocks_of_later_tokens(D):
+    """NaN blocks reach the rows that see their tokens, not earlier rows of the
+    same tile, whole calls and keys shared out."""
+    rng = np.random.default_rng(D)
+    for cached, new in (([0, 30], [150, 100]), ([2500], [90])):
+        end = cached[-1] + new[-1]
+
+        def fill(kind, b, i, shape):
+            x = rng.standard_normal(shape)
+            if b == len(new) - 1:
+                for pos, h, d in ((end - 70, 0, 33), (end - 9, 0, 2), (end - 3, 1, 63)):
+                    if kind == "v" and i == pos // 16:
+                        x[h, pos % 16, d] = np.nan
+                if kind == "k" and i == (end - 5) // 16:
+                    x[1, (end - 5) % 16, 7] = np.inf
+            return x
+        c = Cache(rng, np.add(cached, new), 2, D, fill=fill).to_device()
+        qf, q = bf16(rng.standard_normal((sum(new), 6, D)))
+        qs = dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+        out = torch.empty_like(q)
+        bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, qs, 0.1, out)
+        with np.errstate(invalid="ignore"):
+            ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, new, 0.1)
+        T = sum(new)
+        want = np.zeros(ref.shape, dtype=bool)               # the oracle's own NaNs are those
+        want[T - 70:, :3, 32:64] = want[T - 9:, :3, :32] = want[T - 3:, 3:, 32:64] = want[T - 5:, 3:] = True
+        assert np.array_equal(np.isnan(ref), want)
+        close(out, ref, mag, dot, PROMPT)
+
+
 @pytest.mark.parametrize("spread", [6, 20])
 def test_prompt_values_of_different_sizes(spread):
     rng = np.random.default_rng(spread)
@@ -675,6 +706,52 @@ def test_prompt_then_decode_run():
         ref, mag, dot = kv4.attention(qo.double().cpu().numpy(), *c.pools, c.table, c.lens, new, D ** -0.5)
         close(out, ref, mag, dot, DECODE if new == [1, 1] else PROMPT)
     assert all(np.array_equal(a, b) for a, b in zip(c.bytes(), c.pools)) and bl.device_errors() == 0
+
+
+def test_prompt_graphs_share_the_workspace():
+    """Write, attention and read back of two batches (planned in the waves, and
+    by a launch), a graph each, replayed in turn with eager calls between."""
+    rng = np.random.default_rng(70)
+    H, G, D, rounds = 2, 2, 64, 3
+    kinds = [([40, 3], [37, 70]), (list(rng.integers(0, 60, 70)), list(rng.integers(0, 9, 70)))]
+    sets = []
+    for cached, new in kinds:
+        T = int(sum(new))
+        pair = [Cache(np.random.default_rng(5), cached, H, D, room=rounds * max(new)).to_device() for _ in range(2)]
+        qs = dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+        # five rows that no request owns: left alone
+        x = torch.randn((rounds, T + 5, (G + 2) * H, D), device="cuda").to(torch.bfloat16)
+        outs = [[torch.full((T + 5, n, D), 3.0, dtype=torch.bfloat16, device="cuda") for n in (G * H, H, H)] for _ in range(2)]
+        sets.append((pair, qs, x, outs, x[0].clone(), T))
+
+    def step(c, qs, rows, outs):
+        bl.kv_write(rows[:, G * H:-H], rows[:, -H:], c.k, c.v, c.bt, c.sl, qs)
+        bl.prefill_attention(rows[:, :G * H], c.k, c.v, c.bt, c.sl, qs, 0.1, outs[0])
+        bl.kv_read(c.k, c.v, c.bt, c.sl, qs, outs[1], outs[2])
+    graphs = []
+    for pair, qs, x, outs, cur, T in sets:           # the workspace grows on caches of no use
+        spare = Cache(np.random.default_rng(5), pair[0].lens, H, D, room=99).to_device()
+        step(spare, qs, cur, [torch.empty_like(o) for o in outs[0]])
+    torch.cuda.synchronize()
+    for pair, qs, x, outs, cur, T in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(pair[0], qs, cur, outs[0])
+        graphs.append(g)
+    bl.device_errors()
+    for i in range(rounds):
+        for g, (pair, qs, x, outs, cur, T) in zip(graphs, sets):
+            cur.copy_(x[i])
+            g.replay()
+        for pair, qs, x, outs, cur, T in sets:
+            step(pair[1], qs, x[i], outs[1])
+        torch.cuda.synchronize()
+        for pair, qs, x, outs, cur, T in sets:
+            assert all(torch.equal(a, b) for a, b in zip(*outs)), i
+            assert all((o[T:] == 3).all() for o in outs[0]) and not torch.isnan(outs[0][0]).any()
+            assert all(np.array_equal(a, b) for a, b in zip(pair[0].bytes(), pair[1].bytes())), i
+    assert bl.device_errors() == 1 | 2                    # the rows of no request
+    assert all(torch.equal(p[0].sl, p[1].sl) for p, *_ in sets)
 
 
 def test_another_stream():
