@@ -57,7 +57,7 @@ struct Workspace {
 std::mutex g_ws_mutex;
 Workspace g_ws[kMaxDevices];
 int g_cu_count[kMaxDevices];
-int g_blocks_per_cu[kMaxDevices][3][2][9][3];  // [dev][pool type][D==128][pages per step][depth], 0 = unknown
+int g_blocks_per_cu[kMaxDevices][3][2][5][3];  // [dev][pool type][D==128][pages per step][depth], 0 = unknown
 
 int current_device(int* dev) {
     hipError_t e = hipGetDevice(dev);
@@ -875,7 +875,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t* q, const bellman_tensor_t* k, c
     if (!aligned(positions->data, 4)) return fail(BELLMAN_ERR_UNSUPPORTED, "positions: misaligned data");
     if (H_q < 1 || H_kv < 1) return fail(BELLMAN_ERR_INVALID_ARG, "q and k need a head each");
     if (H_q > 65535 || H_kv > 65535) return fail(BELLMAN_ERR_UNSUPPORTED, "more than 65535 heads");
-    if (T > INT32_MAX / 2) return fail(BELLMAN_ERR_UNSUPPORTED, "too many tokens");
+    // (a token takes a wave; a launch holds fewer than 2^32 threads)
+    if (T >= INT64_C(1) << 26) return fail(BELLMAN_ERR_UNSUPPORTED, "2^26 tokens or more");
     RopeArgs a;
     // axis x turns sections[x] frequencies, in order
     int64_t sum = 0;

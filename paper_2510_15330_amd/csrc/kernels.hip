@@ -1861,7 +1861,7 @@ struct Variant {
 };
 
 // Dispatch on (head_dim, pool type, pages per step, depth): 1 or 2 pages for
-// bf16 pools, 1, 2 or 4 for fp8 pools, depth 1 or 2; 4 or 8 for 4-bit pools, depth 1.
+// bf16 pools, 1, 2 or 4 for fp8 pools, depth 1 or 2; 4 for 4-bit pools, depth 1.
 template <int D, int KV, int PP>
 static int dispatch_depth(int depth, bool occ, const AttnArgs* a, int grid, hipStream_t s) {
     if (depth == 2) {

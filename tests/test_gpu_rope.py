@@ -119,6 +119,17 @@ def test_in_place():
         run(rng, 300, 12, 4, 128, 32, rng.integers(0, 999, 300), inter=inter, qw=torch.bfloat16, kw=torch.bfloat16, in_place=True)
 
 
+def test_rows_past_binary32_are_zero():
+    x = torch.randn((5, 2, 128), device="cuda").to(torch.bfloat16)
+    x[2, 1, 3] = 1e25                                 # its square is infinite
+    w = torch.ones(128, device="cuda")
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    bl.qk_norm_rope(x, x, torch.arange(5, dtype=torch.int32, device="cuda"), torch.logspace(0, -3, 64, device="cuda"), a, b,
+                    q_weight=w)
+    assert not a[2, 1].any() and a[2, 0].all() and not torch.isnan(a).any()
+    assert b[2, 1].abs().max() > 1e24                 # no norm, no squares
+
+
 def test_nan_and_zero_rows_stay_their_own():
     x = torch.randn((6, 3, 64), device="cuda").to(torch.bfloat16)
     x[2, 1, 5] = float("nan")

@@ -242,6 +242,7 @@ def sect(*s, axes=None, **kw):
     (dict(o=B.RopeOpts(float("nan"), 0.0, 0, 1)), ERR_INVALID, "eps"),
     (dict(o=B.RopeOpts(1e-6, float("inf"), 0, 1)), ERR_INVALID, "weight_offset"),
     (dict(o=B.RopeOpts(1e-6, 0.0, 2, 1)), ERR_INVALID, "interleaved"),
+    (rope_args(T=1 << 26), ERR_UNSUPPORTED, "2^26 tokens"),
 ])
 def test_rope_refusals(change, code, text):
     assert call_rope({**rope_args(), **change}) == code
