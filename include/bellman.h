@@ -152,10 +152,10 @@ int bellman_kv_append(const bellman_tensor_t *k_new, const bellman_tensor_t *v_n
  *   out          bf16 [B, H_q, D], innermost contiguous (written; rounded to
  *                nearest even).  A request of length 0 gets zeros.
  * Over 4-bit pools the keys enter the matrix cores as they lie (a score is off
- * by at most 2^-13 of its sum of |products|); the values'
- * scales go into the weights, held as the sum of two bf16 (2^-14 relative),
- * whose scaled magnitudes below 2^-126 count as 0.  A NaN key block makes its
- * (request, head)'s rows NaN, a NaN value block its 32 dims of them.
+ * by at most 2^-13 of its sum of |products|); the values' scales go into the
+ * weights, held as the sum of two bf16 (2^-14 relative), whose scaled
+ * magnitudes below 2^-126 count as 0.  A NaN key block makes its (request,
+ * head)'s rows NaN, a NaN value block its 32 dims of them.
  * The work of the batch, as (request, KV head, step of consecutive pages)
  * units, is dealt to the GPU's resident wavefronts in equal contiguous
  * shares; a request cut by a share boundary has its partial softmax

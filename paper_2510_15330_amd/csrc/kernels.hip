@@ -702,7 +702,9 @@ __device__ __forceinline__ void fp8_step(AttnState<D>& st, const PageK<D, true> 
 
 // ------------------------------------------------- 4-bit pages on MFMA ---
 // A page of one head is a tile of 17 D / 2 bytes: 8 D bytes of e2m1 codes and
-// D / 2 E8M0 scales, one for every 32 dims of a token (bellman.h).
+// D / 2 E8M0 scales, one for every 32 dims of a token (bellman.h).  Bound by the
+// page stream: 256 requests of 6-13.5k tokens, 8 heads of 128, 2.73 GB, in
+// 447-466 us (5.9-6.1 TB/s); the loads without the arithmetic took 444-459.
 //
 // QK: the matrix cores take K as it lies.  In v_mfma_scale_f32_16x16x128_f8f6f4
 // with A in e2m1, lane (qg, n) supplies row n at k = 32 qg .. 32 qg + 31 with
@@ -710,18 +712,18 @@ __device__ __forceinline__ void fp8_step(AttnState<D>& st, const PageK<D, true> 
 // in e4m3 takes k = 16 qg + 0..15 and 64 + 16 qg + 0..15 from lane (qg, n): the
 // order of the query terms hi + lo that the fp8 pools use (every bf16 within
 // 2^-14 of its row's largest is exact in the two; the instruction aligns the
-// products of a few neighbouring dims, keeping 13 bits below the largest).  At head_dim 64 a product
-// holds two pages: lane groups 0, 1 (k < 64) the even one, groups 2, 3 the odd
-// one, and the query terms lie in the lower or the upper k half.
+// products of a few neighbouring dims, keeping 13 bits below the largest).  At
+// head_dim 64 a product holds two pages: lane groups 0, 1 (k < 64) the even one,
+// groups 2, 3 the odd one, and the query terms lie in the lower or the upper k
+// half.
 //
 // PV: codes widen exactly to bf16 (A, 16 dims x 32 tokens of a page pair).  The
 // scale of a value depends on its token and 32-dim block, so it goes into the
 // weights: the product of block b takes p 2^(s - 127), as a sum of two bf16 (hi
 // truncated, lo the remainder: 2^-14 relative).  Weights are held 2^127 times
-// as large, so a scaled
-// weight's bf16 bits are the weight's less (254 - s) << 7, one saturating 16-bit
-// subtraction for two values; what falls below 2^-126 becomes 0 or below
-// 2^-126.
+// as large, so a scaled weight's bf16 bits are the weight's less (254 - s) << 7,
+// one saturating 16-bit subtraction for two values; what falls below 2^-126
+// becomes 0 or below 2^-126.
 //
 // Scales go through LDS: each lane loads its share of the step's scale bytes (a
 // 64 / PP lanes' worth of words a page), forms the subtrahends of its V scales
@@ -1124,8 +1126,8 @@ attn_mfma_kernel(AttnArgs a) {
     // lines a tile at head_dim 128, 4.25 at 64), which are then in flight
     // together (256 requests of 6-13.5k tokens 477 -> 470 us, 512 with Zipf
     // lengths to 8k 194 -> 187; with the scales' loads not streamed 457 and
-    // 184, all loads not streamed 504 and 195).  Wave v of the plan, and of the pieces: the waves of
-    // one head of the groups, one after the other.
+    // 184, all loads not streamed 504 and 195).  Wave v of the plan, and of the
+    // pieces: the waves of one head of the groups, one after the other.
     const int hs = FP4 ? a.hs : 1;
     const int wg = FP4 ? w / hs : w;
     const int g0 = FP4 ? w % hs : 0;
