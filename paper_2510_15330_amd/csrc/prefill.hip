@@ -248,14 +248,14 @@ __global__ void lens_kernel(WriteArgs a) {
 }
 
 // ------------------------------------------------------ 4-bit page write --
-// A wave takes a page of one head at a time.  Lane (blk, tok) quantises 32
-// dims of a token (bellman.h has the rule; the scaling is by powers of two, so
-// the bytes are determined) and so has K's 16 bytes and scale as they lie in
-// the tile.  V lies by 4-slot groups: the lanes' code words go through LDS,
-// and lane (q, n) gathers dims 16 t + n of slots 4q..4q+3 into its own 16
-// bytes.  Bytes of V that hold slots outside the request's new rows keep those
-// slots' codes.  Bound by memory: rows read once, the tile written once (37,461
-// tokens of 8 heads of 128, 193 MB, 34 us, 5.6 TB/s).
+// A wave takes a page of one head at a time, D / 8 lanes a row: a lane quantises
+// 8 dims, four lanes a block (bellman.h has the rule; the scaling is by powers of
+// two, so the bytes are determined).  The code words go through LDS: K's leave as
+// 16 bytes a (block, slot), and lane (q, n) gathers V's dims 16 t + n of slots
+// 4q..4q+3 into its own 16 bytes.  Bytes of V that hold slots outside the
+// request's new rows keep those slots' codes.  Bound by memory: rows read once,
+// the tile written once (37,461 tokens of 8 heads of 128, 193 MB, 39-41 us, 4.7-5
+// TB/s; with 32 dims a lane, whose loads touch twice the lines, 45-47).
 constexpr uint32_t kNan4 = 255u;
 
 // The scale byte of a block whose largest magnitude has the bf16 bits m.
@@ -264,31 +264,30 @@ __device__ __forceinline__ uint32_t scale4(uint32_t m) {
     return m >= 0x7f80u ? kNan4 : (uint32_t)min(max((int)((m + 0x1fu) >> 7) - 2, 0), 252);
 }
 
-// 16 words of bf16 pairs -> 32 codes in 4 words, and the scale byte.
-__device__ __forceinline__ uint32_t quantize4(const uint32_t (&in)[16], u32x4& codes) {
+// Eight bf16 values of a block that four neighbouring lanes hold: their codes,
+// and the block's scale byte.
+__device__ __forceinline__ uint32_t quantize8(const u32x4& in, uint32_t& scale) {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-    u16x2 m = {0, 0};
+    u16x2 m2 = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, in[i] & 0x7fff7fffu));
-    const uint32_t s = scale4(max((uint32_t)m.x, (uint32_t)m.y));
-    const float inv = __uint_as_float((254u - min(s, 252u)) << 23);
+    for (int i = 0; i < 4; ++i)
+        m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(u16x2, in[i] & 0x7fff7fffu));
+    uint32_t m = max((uint32_t)m2.x, (uint32_t)m2.y);
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));   // lane ^ 1
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true));   // lane ^ 2
+    scale = scale4(m);
+    const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);
+    float lo[4], hi[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t w = 0;
-        const float lo[4] = {__uint_as_float(in[4 * i] << 16) * inv, __uint_as_float(in[4 * i + 1] << 16) * inv,
-                             __uint_as_float(in[4 * i + 2] << 16) * inv, __uint_as_float(in[4 * i + 3] << 16) * inv};
-        const float hi[4] = {__uint_as_float(in[4 * i] & 0xffff0000u) * inv,
-                             __uint_as_float(in[4 * i + 1] & 0xffff0000u) * inv,
-                             __uint_as_float(in[4 * i + 2] & 0xffff0000u) * inv,
-                             __uint_as_float(in[4 * i + 3] & 0xffff0000u) * inv};
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[0], hi[0], 1.0f, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[1], hi[1], 1.0f, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[2], hi[2], 1.0f, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[3], hi[3], 1.0f, 3);
-        codes[i] = s == kNan4 ? 0u : w;
+        lo[i] = __uint_as_float(in[i] << 16) * inv;
+        hi[i] = __uint_as_float(in[i] & 0xffff0000u) * inv;
     }
-    return s;
+    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, lo[0], hi[0], 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[1], hi[1], 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[2], hi[2], 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, lo[3], hi[3], 1.0f, 3);
+    return scale == kNan4 ? 0u : w;
 }
 
 __device__ __forceinline__ void wave_lds_fence() {   // one wave's LDS writes before its other lanes' reads
@@ -297,10 +296,12 @@ __device__ __forceinline__ void wave_lds_fence() {   // one wave's LDS writes be
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-template <int D>
+template <int D, bool STREAM>
 __global__ void __launch_bounds__(256) kv4_write_kernel(WriteArgs a, const int32_t* page_start) {
-    // [token][dim / 8 mod 2][dim / 16] code words, a row padded to spread the banks
-    constexpr int ROW = D / 8 + 4;
+    constexpr int RL = D / 8, RP = 64 / RL, NI = kPage / RP;     // lanes a row, rows a load, loads a tensor
+    // code words, rows padded to spread the banks: K [token][dim / 8], V [token][dim / 8 mod 2][dim / 16]
+    constexpr int ROW = RL + 4;
+    __shared__ __attribute__((aligned(16))) uint32_t kst[4][kPage * ROW];
     __shared__ __attribute__((aligned(16))) uint32_t vst[4][kPage * ROW];
     const int lane = threadIdx.x & 63, n = lane & 15, qg = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -317,45 +318,36 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(WriteArgs a, const int32
     }
     const int64_t row0 = it.s0 + (first - it.L);            // token row of slot 0
     constexpr int TB = kTile4Rows * D / 2;
-    const int blk = D == 128 ? qg : qg & 1;
-    const bool live = n >= slot_lo && n < slot_hi;
+    const int r0 = lane / RL, c = lane % RL;
+    auto live = [&](int slot) { return slot >= slot_lo && slot < slot_hi; };
     for (int g = blockIdx.y * 4 + w; g < a.H_kv; g += 4 * gridDim.y) {
         char* kp = (char*)a.k_pages + ((int64_t)pg * a.H_kv + g) * TB;
         char* vp = (char*)a.v_pages + ((int64_t)pg * a.H_kv + g) * TB;
-        const uint16_t* kn = (const uint16_t*)a.k_new + (row0 + n) * a.k_st + (int64_t)g * a.k_sh + 32 * blk;
-        const uint16_t* vn = (const uint16_t*)a.v_new + (row0 + n) * a.v_st + (int64_t)g * a.v_sh + 32 * blk;
-        constexpr int NP = D == 128 ? 2 : 1;    // head_dim 64: lanes 0-31 take K, 32-63 V
-        uint32_t in[NP][16];
+        const uint16_t* kn = (const uint16_t*)a.k_new + row0 * a.k_st + (int64_t)g * a.k_sh + 8 * c;
+        const uint16_t* vn = (const uint16_t*)a.v_new + row0 * a.v_st + (int64_t)g * a.v_sh + 8 * c;
+        u32x4 kin[NI], vin[NI];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const uint16_t* src = (D == 128 ? p == 1 : lane >= 32) ? vn : kn;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32x4 x = live ? *(const u32x4*)(src + 8 * i) : u32x4{0u, 0u, 0u, 0u};
-                in[p][4 * i] = x.x;
-                in[p][4 * i + 1] = x.y;
-                in[p][4 * i + 2] = x.z;
-                in[p][4 * i + 3] = x.w;
-            }
+        for (int i = 0; i < NI; ++i) {
+            const int slot = i * RP + r0;
+            auto load = [&](const uint16_t* p) {
+                return STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
+            };
+            kin[i] = live(slot) ? load(kn + slot * a.k_st) : u32x4{0u, 0u, 0u, 0u};
+            vin[i] = live(slot) ? load(vn + slot * a.v_st) : u32x4{0u, 0u, 0u, 0u};
         }
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const bool isv = D == 128 ? p == 1 : lane >= 32;
-            u32x4 c;
-            const uint32_t s = quantize4(in[p], c);
-            if (!isv) {
-                if (live) {
-                    *(u32x4*)(kp + blk * 256 + n * 16) = c;
-                    *(uint8_t*)(kp + 8 * D + blk * 16 + n) = (uint8_t)s;
-                }
-            } else {
-                if (live) *(uint8_t*)(vp + 8 * D + (n >> 2) * (D / 8) + 4 * blk + (n & 3)) = (uint8_t)s;
-                uint32_t* row = &vst[w][n * ROW];
-                *(u32x2*)(row + 2 * blk) = u32x2{c.x, c.z};
-                *(u32x2*)(row + D / 16 + 2 * blk) = u32x2{c.y, c.w};
+        for (int i = 0; i < NI; ++i) {
+            const int slot = i * RP + r0;
+            uint32_t ks, vs;
+            kst[w][slot * ROW + c] = quantize8(kin[i], ks);
+            vst[w][slot * ROW + (c & 1) * (D / 16) + (c >> 1)] = quantize8(vin[i], vs);
+            if ((c & 3) == 0 && live(slot)) {
+                *(uint8_t*)(kp + 8 * D + (c >> 2) * 16 + slot) = (uint8_t)ks;
+                *(uint8_t*)(vp + 8 * D + (slot >> 2) * (D / 8) + (c & ~3) + (slot & 3)) = (uint8_t)vs;
             }
         }
         wave_lds_fence();
+        if ((D == 128 || lane < 32) && live(n)) *(u32x4*)(kp + lane * 16) = *(const u32x4*)&kst[w][n * ROW + 4 * qg];
         // lane (q, n): dims 16 t + n of slots 4q .. 4q + 3, nibble r of halfword t
         const int q = qg, sh = 4 * (n & 7);
         uint32_t o[D / 32];
@@ -1853,8 +1845,13 @@ void launch_kv_write(const WriteArgs& a, int32_t* page_start, hipStream_t s) {
     const dim3 grid(items, ny);
     if (a.kv == kKvFp4) {
         const dim3 g4(items, std::min((unsigned)(a.H_kv + 3) / 4, ny));   // a wave a head
-        if (a.D == 128) hipLaunchKernelGGL(kv4_write_kernel<128>, g4, dim3(256), 0, s, a, (const int32_t*)page_start);
-        else hipLaunchKernelGGL(kv4_write_kernel<64>, g4, dim3(256), 0, s, a, (const int32_t*)page_start);
+        // Rows of more than half the 256 MB memory-side cache are streamed past it:
+        // written and read back, 37k tokens of 8 heads of 128 (153 MB of rows) 75 us,
+        // 83 through it; of 64 (77 MB) 43.5 us, 41.6 through it.
+        const bool stream = (int64_t)a.T * a.H_kv * a.D * 4 > (128 << 20);
+        const auto kernel = a.D == 128 ? (stream ? kv4_write_kernel<128, true> : kv4_write_kernel<128, false>)
+                                       : (stream ? kv4_write_kernel<64, true> : kv4_write_kernel<64, false>);
+        hipLaunchKernelGGL(kernel, g4, dim3(256), 0, s, a, (const int32_t*)page_start);
     } else if (a.elem_bytes == 2) {
         hipLaunchKernelGGL(kv_write_kernel<2>, grid, dim3(256), 0, s, a, (const int32_t*)page_start);
     } else {

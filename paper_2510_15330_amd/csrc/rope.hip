@@ -3,8 +3,8 @@
 // R(p) turning each pair of the first R dims by position times frequency.
 //
 // Bound by memory: (H_q + H_kv) D values a token read and written once (36,001
-// tokens of 32/8 heads of 128, 737 MB, in 137-141 us, 5.2-5.4 TB/s; 4,613 of 28/4
-// in 16.1 us; 64 tokens 4.1 us, a launch's latency).  Six waves a SIMD (68
+// tokens of 32/8 heads of 128, 737 MB, in 128 us, 5.8 TB/s; 4,613 of 28/4 in
+// 15.8 us; 64 tokens 4.1 us, a launch's latency).  Six waves a SIMD (68
 // registers; at four, 8,000 tokens of 64 dims took 23 us instead of 17.4, and
 // loads a pass ahead cost more registers than they hid).  A row
 // is D / 16 lanes, each with two 16-byte units whose values pair up (dims i and
@@ -57,7 +57,8 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-template <int D, bool INTER>
+// STREAM: the stores (1) or loads and stores (2) pass the caches by.
+template <int D, bool INTER, int STREAM>
 __global__ void __launch_bounds__(256, 6) qk_norm_rope_kernel(RopeArgs a) {
     constexpr int LPR = D / 16, RPW = 64 / LPR;     // lanes a row, rows a pass
     const int lane = threadIdx.x & 63, j = lane % LPR, sub = lane / LPR;
@@ -98,7 +99,14 @@ __global__ void __launch_bounds__(256, 6) qk_norm_rope_kernel(RopeArgs a) {
         const int H = isk ? a.H_kv : a.H_q;
         const int row = (isk ? p - pq : p) * RPW + sub, h = min(row, H - 1);
         const uint16_t* src = isk ? a.k + t * a.k_st + (int64_t)h * a.k_sh : a.q + t * a.q_st + (int64_t)h * a.q_sh;
-        const u32x4 xa = *(const u32x4*)(src + ua), xb = *(const u32x4*)(src + ub);
+        u32x4 xa, xb;
+        if (STREAM == 2) {
+            xa = __builtin_nontemporal_load((const u32x4*)(src + ua));
+            xb = __builtin_nontemporal_load((const u32x4*)(src + ub));
+        } else {
+            xa = *(const u32x4*)(src + ua);
+            xb = *(const u32x4*)(src + ub);
+        }
         const void* wp = isk ? a.k_weight : a.q_weight;
         if (wp && have != (int)isk) {
             have = (int)isk;
@@ -145,8 +153,13 @@ __global__ void __launch_bounds__(256, 6) qk_norm_rope_kernel(RopeArgs a) {
         }
         if (row < H) {
             uint16_t* dst = isk ? a.k_out + t * a.ko_st + (int64_t)h * a.ko_sh : a.q_out + t * a.qo_st + (int64_t)h * a.qo_sh;
-            *(u32x4*)(dst + ua) = ya;
-            *(u32x4*)(dst + ub) = yb;
+            if (STREAM) {
+                __builtin_nontemporal_store(ya, (u32x4*)(dst + ua));
+                __builtin_nontemporal_store(yb, (u32x4*)(dst + ub));
+            } else {
+                *(u32x4*)(dst + ua) = ya;
+                *(u32x4*)(dst + ub) = yb;
+            }
         }
     }
 }
@@ -162,13 +175,22 @@ void launch_qk_norm_rope(const RopeArgs& args, hipStream_t s) {
     // (2048 tokens of 32/8 heads of 128: 11.9 us at 4096, 12.8 at 8192).
     a.chunks = (int)std::min<int64_t>(passes, (4096 + a.T - 1) / a.T);
     const dim3 grid((unsigned)(((int64_t)a.T * a.chunks + 3) / 4));
-    if (a.D == 128) {
-        if (a.interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((qk_norm_rope_kernel<128, false>), grid, dim3(256), 0, s, a);
-    } else {
-        if (a.interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<64, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((qk_norm_rope_kernel<64, false>), grid, dim3(256), 0, s, a);
-    }
+    // Streamed (stores; loads and stores / neither, us; rows of 32/8 heads): stores
+    // of pairs (i, i + F) at head_dim 128, where an instruction writes whole lines:
+    // 2,048 tokens 8.8 / 10.8, 8,000 29.9 / 30.1, 20,000 65 / 82.  The others once
+    // input and output pass the 256 MB memory-side cache: head_dim 64 20,000 37.7 /
+    // 34.1, 72,000 137 / 144, neighbouring pairs 9,000 of 28/4 31 / 28, 20,000 77 /
+    // 87.  The loads too, of whole lines, once the input alone is well past it:
+    // 30,000 107 / 105 with stores alone, 33,000 118 / 122, 60,000 210 / 225.
+    const int64_t in = (int64_t)a.T * (a.H_q + a.H_kv) * a.D * 2;
+    const bool lines = a.D == 128 && !a.interleaved;
+    const int stream = lines ? 1 + (a.R == a.D && in > (320 << 20)) : 2 * in > (256 << 20);
+    const auto kernel =
+        a.D == 128 ? (a.interleaved ? (stream ? qk_norm_rope_kernel<128, true, 1> : qk_norm_rope_kernel<128, true, 0>)
+                                    : (stream == 2 ? qk_norm_rope_kernel<128, false, 2> : qk_norm_rope_kernel<128, false, 1>))
+                   : (a.interleaved ? (stream ? qk_norm_rope_kernel<64, true, 1> : qk_norm_rope_kernel<64, true, 0>)
+                                    : (stream ? qk_norm_rope_kernel<64, false, 1> : qk_norm_rope_kernel<64, false, 0>));
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
 }
 
 }  // namespace bellman

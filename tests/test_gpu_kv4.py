@@ -271,6 +271,36 @@ def test_read_of_malformed_requests():
         assert bl.device_errors() & 2 and (ko == 5).all()
 
 
+@pytest.mark.parametrize("H,D", [(8, 128), (17, 64)])
+def test_rows_past_the_cache_are_written_as_fewer_are(H, D):
+    """More than 128 MB of rows (streamed), and the same in three calls."""
+    n = [20000, 1, 14007]
+    rng = np.random.default_rng(D)
+    need = [(x + 15) // 16 for x in n]
+    NP = sum(need)
+    bt = np.full((3, max(need)), -1, dtype=np.int32)
+    for b, (k, perm) in enumerate(zip(need, np.split(rng.permutation(NP).astype(np.int32), np.cumsum(need)[:2]))):
+        bt[b, :k] = perm
+    bt = dev(bt)
+    g = torch.Generator("cuda").manual_seed(D)
+    k, v = (torch.randn((sum(n), H, D), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    assert k.numel() * 4 > 128 << 20
+    at, pools = np.concatenate([[0], np.cumsum(n)]), []
+    for parts in (1, 3):
+        p = [torch.zeros((NP, H, 17, D // 2), dtype=torch.uint8, device="cuda").view(F4) for _ in range(2)]
+        sl = torch.zeros(3, dtype=torch.int32, device="cuda")
+        if parts == 1:
+            bl.kv_write(k, v, *p, bt, sl, dev(at.astype(np.int32)))
+        else:
+            for b in range(3):
+                s = slice(int(at[b]), int(at[b + 1]))
+                bl.kv_write(k[s], v[s], *p, bt[b:b + 1], sl[b:b + 1], dev(np.array([0, n[b]], dtype=np.int32)))
+        assert sl.tolist() == n
+        pools.append([x.view(torch.uint8) for x in p])
+    assert bl.device_errors() == 0
+    assert all(torch.equal(a, b) and a.any() for a, b in zip(*pools))
+
+
 # ----------------------------------------------------------------- decode --
 
 SHAPES = [  # H_q, H_kv, D, lengths

@@ -119,6 +119,28 @@ def test_in_place():
         run(rng, 300, 12, 4, 128, 32, rng.integers(0, 999, 300), inter=inter, qw=torch.bfloat16, kw=torch.bfloat16, in_place=True)
 
 
+@pytest.mark.parametrize("T,H_q,H,D,F,inter", [(36001, 32, 8, 128, 64, False), (17000, 32, 8, 128, 48, False),
+                                               (17000, 32, 8, 128, 64, True), (30011, 40, 8, 64, 32, False),
+                                               (30011, 40, 8, 64, 16, True)])
+def test_many_tokens_are_as_few(T, H_q, H, D, F, inter):
+    """Rows past the memory-side cache (streamed), and the same in parts that fit, bit for bit."""
+    g = torch.Generator("cuda").manual_seed(T + D)
+    x = torch.randn((T, H_q + H, D), generator=g, device="cuda").to(torch.bfloat16)
+    q, k = x[:, :H_q], x[:, H_q:]
+    pos = torch.randint(0, 100000, (T,), generator=g, device="cuda", dtype=torch.int32)
+    inv, w = torch.logspace(0, -4, F, device="cuda"), torch.rand(D, generator=g, device="cuda").to(torch.bfloat16)
+    outs = []
+    for step in (T, 5001):
+        qo, ko = torch.full((T, H_q, D), 3.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, H, D), 3.0, dtype=torch.bfloat16, device="cuda")
+        for i in range(0, T, step):
+            s = slice(i, min(i + step, T))
+            bl.qk_norm_rope(q[s], k[s], pos[s], inv, qo[s], ko[s], q_weight=w, k_weight=w, interleaved=inter)
+        outs.append((qo, ko))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    bl.qk_norm_rope(q, k, pos, inv, q, k, q_weight=w, k_weight=w, interleaved=inter)      # in place
+    assert torch.equal(q, outs[0][0]) and torch.equal(k, outs[0][1])
+
+
 def test_rows_past_binary32_are_zero():
     x = torch.randn((5, 2, 128), device="cuda").to(torch.bfloat16)
     x[2, 1, 3] = 1e25                                 # its square is infinite
