@@ -170,14 +170,15 @@ void launch_qk_norm_rope(const RopeArgs& args, hipStream_t s) {
     RopeArgs a = args;
     const int rpw = 64 / (a.D / 16);
     const int passes = (a.H_q + rpw - 1) / rpw + (a.H_kv + rpw - 1) / rpw;
-    // A token's passes go over as many waves as it takes to have 4096 (four a
-    // SIMD); from 4096 tokens on one wave takes a token and forms its angles once
-    // (2048 tokens of 32/8 heads of 128: 11.9 us at 4096, 12.8 at 8192).
-    a.chunks = (int)std::min<int64_t>(passes, (4096 + a.T - 1) / a.T);
+    // A token's passes go over as many waves as it takes to have 2048 (two a SIMD);
+    // from 2048 tokens on one wave takes a token and forms its angles once (for
+    // 1024, 2048, 4096 waves, us: 1,024 tokens of 32/8 heads of 128 7.0, 6.5, 7.1,
+    // 2,048 8.4, 8.3, 8.9, 256 5.3, 5.1, 5.1).
+    a.chunks = (int)std::min<int64_t>(passes, (2048 + a.T - 1) / a.T);
     const dim3 grid((unsigned)(((int64_t)a.T * a.chunks + 3) / 4));
     // Streamed (stores; loads and stores / neither, us; rows of 32/8 heads): stores
     // of pairs (i, i + F) at head_dim 128, where an instruction writes whole lines:
-    // 2,048 tokens 8.8 / 10.8, 8,000 29.9 / 30.1, 20,000 65 / 82.  The others once
+    // 2,048 tokens 8.4 / 10.8, 8,000 29.9 / 30.1, 20,000 65 / 82.  The others once
     // input and output pass the 256 MB memory-side cache: head_dim 64 20,000 37.7 /
     // 34.1, 72,000 137 / 144, neighbouring pairs 9,000 of 28/4 31 / 28, 20,000 77 /
     // 87.  The loads too, of whole lines, once the input alone is well past it:
