@@ -1,5 +1,6 @@
 """MI355X (gfx950) paged decode attention with beLLMan's length controller,
-and the prompt (prefill) path that fills the cache before decoding.
+the prompt (prefill) path that fills the cache before decoding, and the norm
+and rotation of queries and keys before it.  Pools in bf16, fp8 or 4 bits.
 
 The numerical work runs in ``libbellman.so`` (HIP kernels behind a C ABI,
 declared in ``include/bellman.h``); this package marshals torch tensors into

@@ -339,7 +339,8 @@ def decode_step(k_new, v_new, q, k_pages, v_pages, block_table, seq_lens, scale,
                 k_scale=None, v_scale=None, max_waves=0, xcd_skew=0, events=None, pages_per_step=0,
                 pipeline_depth=0, wave_times=None):
     """bellman_decode_step: kv_append of (k_new, v_new) and decode_attention
-    of q in one call (the append fused into the attention launch)."""
+    of q in one call (the append fused into the attention launch; over 4-bit
+    pools two launches)."""
     _device_tensors(k_new, v_new, q, k_pages, v_pages, block_table, seq_lens, out, k_scale, v_scale, wave_times)
     ev0 = ev1 = None
     if events is not None:
@@ -368,7 +369,8 @@ def probe_gather(pool, tile_bytes, sink, max_waves=0, stream=None):
 
 def kv_write(k_new, v_new, k_pages, v_pages, block_table, seq_lens, q_start, stream=None):
     """bellman_kv_write: write each request's new prompt tokens after its
-    cached ones, then seq_lens += tokens written."""
+    cached ones (bf16 rows into 4-bit pools, torch.float4_e2m1fn_x2 [NP, H_kv,
+    17, D/2], are quantised), then seq_lens += tokens written."""
     if _call("kv_write", _WRITE, stream, 0.0, 0, None, None, k_new, v_new, k_pages, v_pages, block_table, seq_lens,
              q_start):
         return
