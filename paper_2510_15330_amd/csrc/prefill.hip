@@ -1056,6 +1056,7 @@ __global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
 // (computed one step earlier), then issues the MFMAs of S(s + 1)
 // interleaved with the exponentials of P(s), then the PV MFMAs of step s.
 constexpr float kLazyMax = 8.0f;
+constexpr float kFarMax = 4194304.f;   // 2^22: below it m is within 2^-3 of the score it was rounded from
 // bf16 pools: O is held at a scale 2^eref, never coarser than the step at
 // hand, so that no weight is made smaller before it is rounded to fp16 (whose
 // numbers below 2^-14 lose a bit a factor of two): O moves up to a finer
@@ -1258,6 +1259,7 @@ prefill_attn_kernel(PrefillArgs a) {
     // m starts at the lowest finite value: scores of -inf alone weigh nothing
     // (l = 0), and only a NaN makes l one
     float m = -__FLT_MAX__, l = 0.f;
+    float m_lazy = m + kLazyMax;   // O and l are rescaled where the max passes this
     bool bad = false;
 
     // the block-table entries (and value scales) of WIN steps at a time sit in
@@ -1596,18 +1598,34 @@ prefill_attn_kernel(PrefillArgs a) {
                 for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[hh][j]);
             mx = fmaxf(mx, swap_halves(mx));
             const float m_new = fmaxf(m, mx * sl);     // scaled units
-            if (__any(m_new > m + kLazyMax)) {
+            float md = FP8 ? m : m + d;
+            if (__any(m_new > m_lazy)) {
                 const float alpha = __builtin_amdgcn_exp2f(m - m_new);
                 l *= alpha;
 #pragma unroll
                 for (int t = 0; t < D / 32; ++t) o[t] *= alpha;
                 m = m_new;
+                // The weights' exponents are sc sl - md in one rounding.  In a
+                // column whose m is far from 0 the rounding of the product in m,
+                // and of m + d, would be whole powers of two of P: there the
+                // scaled scores less m are taken first (every step comes here),
+                // over sl, exact to 2^-22 of the few units that matter.
+                const bool far = !(fabsf(m) < kFarMax);
+                m_lazy = far ? -INFINITY : m + kLazyMax;
+                md = FP8 ? (far ? 0.f : m) : (far ? d : m + d);
+                if (__any(far)) {
+#pragma clang fp contract(off)      // the product rounded, as in m
+                    const float inv = 1.f / sl;
+#pragma unroll
+                    for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sc[hh][j] = far ? (sc[hh][j] * sl - m) * inv : sc[hh][j];
+                }
             }
             // S of step s + 1 on the matrix cores while P of step s is formed
             // (past a wave's last step the result is not used)
             qk(k_rd, scn);
             float psum = 0.f;
-            const float md = FP8 ? m : m + d;
 #pragma unroll
             for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
