@@ -151,8 +151,11 @@ int bellman_kv_append(const bellman_tensor_t *k_new, const bellman_tensor_t *v_n
  *   scale        finite fp32 softmax scale (usually 1/sqrt(D)).
  *   out          bf16 [B, H_q, D], innermost contiguous (written; rounded to
  *                nearest even).  A request of length 0 gets zeros.
- * Over 4-bit pools the keys enter the matrix cores as they lie (a score is off
- * by at most 2^-13 of its sum of |products|); the values' scales go into the
+ * Over 4-bit pools the keys enter the matrix cores as they lie, against the
+ * query as two e4m3 terms with a scale for every 32 dims: a score is off by at
+ * most 2^-13 of its sum of |products|, and by 2^-21 of the sum over 32-dim
+ * blocks of the query's largest magnitude times the key's magnitudes (query dims
+ * below 2^-14 of their block's largest lose bits).  The values' scales go into the
  * weights, held as the sum of two bf16 (2^-14 relative), whose scaled
  * magnitudes below 2^-126 count as 0.  A NaN key block makes its (request,
  * head)'s rows NaN, a NaN value block its 32 dims of them.
@@ -419,8 +422,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * codes are staged in LDS as bytes and widened exactly at the operand load
  * (K to bf16, V to fp16); the K scale folds into the softmax scale and the
  * V scale into the final normalisation.  Over 4-bit pools the keys enter the
- * matrix cores as they lie, against the query as two e4m3 terms (scores as in the
- * decode attention), and the values are copied to fp16 as over
+ * matrix cores as they lie, against the query as two e4m3 terms (scores within
+ * the decode attention's bound), and the values are copied to fp16 as over
  * bf16 pools; a page outside the pool makes the rows that see it NaN, a NaN
  * key block the (request, head)'s rows that see its token, a NaN value block
  * its 32 dims of them.  Scratch

@@ -710,9 +710,10 @@ __device__ __forceinline__ void fp8_step(AttnState<D>& st, const PageK<D, true> 
 // with A in e2m1, lane (qg, n) supplies row n at k = 32 qg .. 32 qg + 31 with
 // one E8M0 scale: slot n's block qg, 16 bytes and a scale byte of the tile.  B
 // in e4m3 takes k = 16 qg + 0..15 and 64 + 16 qg + 0..15 from lane (qg, n): the
-// order of the query terms hi + lo that the fp8 pools use (every bf16 within
-// 2^-14 of its row's largest is exact in the two; the instruction aligns the
-// products of a few neighbouring dims, keeping 13 bits below the largest).  At
+// order of the query terms hi + lo that the fp8 pools use, here with a scale for
+// each 32 dims (every bf16 within 2^-14 of its block's largest is exact in the
+// two, smaller ones are within 2^-21 of that; the instruction aligns the products
+// of a few neighbouring dims, keeping 13 bits below the largest).  At
 // head_dim 64 a product holds two pages: lane groups 0, 1 (k < 64) the even one,
 // groups 2, 3 the odd one, and the query terms lie in the lower or the upper k
 // half.
@@ -757,28 +758,56 @@ __device__ __forceinline__ Scales4<D, PP>& scale_store() {
 }
 
 // The query terms as B operands: [0] (and at head_dim 64 [1], moved to the
-// upper k half for the odd pages).
+// upper k half for the odd pages), and their scales (lo's 2^-4 of hi's).
 template <int D>
 struct Q4 {
     i32x8 hi[D == 128 ? 1 : 2], lo[D == 128 ? 1 : 2];
     int s_hi, s_lo;
 };
-// flip: the sign bits that a negative softmax scale turns
+// Each 32-dim block of a row is scaled for itself, as its keys are: by 2^k, its
+// largest magnitude into [2^7, 2^8).  (One scale a row instead lost the dims
+// 2^-22 below the row's largest, whose keys may be as much larger.)  Lane (qg, n)
+// holds 16 dims of block qg / 2, and at head_dim 128 16 of block 2 + qg / 2; the
+// instruction takes from it the scale of k = 32 qg .. 32 qg + 31.  flip: the sign
+// bits that a negative softmax scale turns.
 template <int D>
 __device__ __forceinline__ void q_to_fp4(const bf16x8 (&bq)[D / 32], Q4<D>& q4, uint32_t flip) {
-    bf16x8 q[D / 32];
+    constexpr int NH = D / 64;
+    uint32_t hw[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u}, lw[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    int k[NH];
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) q[j] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, bq[j]) ^ flip);
-    Q8 q8;
-    q_to_fp8<D>(q, q8);
-    q4.hi[0] = q8.hi;
-    q4.lo[0] = q8.lo;
-    if constexpr (D == 64) {
-        q4.hi[1] = i32x8{0, 0, 0, 0, q8.hi[0], q8.hi[1], q8.hi[2], q8.hi[3]};
-        q4.lo[1] = i32x8{0, 0, 0, 0, q8.lo[0], q8.lo[1], q8.lo[2], q8.lo[3]};
+    for (int h = 0; h < NH; ++h) {
+        u32x4 w[2];
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w[j] = __builtin_bit_cast(u32x4, bq[2 * h + j]) ^ flip;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = max(m, max(w[j][i] & 0x7fffu, (w[j][i] >> 16) & 0x7fffu));
+        }
+        const auto pair = __builtin_amdgcn_permlane16_swap(m, m, false, false);   // the block's other half
+        m = max((uint32_t)pair[0], (uint32_t)pair[1]);
+        k[h] = max(-120, min(134 - (int)(m >> 7), 120));
+        const float sq = __uint_as_float((uint32_t)(k[h] + 127) << 23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w0 = w[i >> 1][2 * (i & 1)], w1 = w[i >> 1][2 * (i & 1) + 1];
+            const float t[4] = {__uint_as_float(w0 << 16) * sq, __uint_as_float(w0 & 0xffff0000u) * sq,
+                                __uint_as_float(w1 << 16) * sq, __uint_as_float(w1 & 0xffff0000u) * sq};
+            split4(t, hw[4 * h + i], lw[4 * h + i]);
+        }
     }
-    q4.s_hi = q8.s_hi;
-    q4.s_lo = q8.s_lo;
+    // block qg's k (at head_dim 64 block qg % 2's): the half swap leaves blocks 0, 0,
+    // 2, 2 and 1, 1, 3, 3 in the lane groups (0, 0, 0, 0 and 1, 1, 1, 1)
+    const auto half = __builtin_amdgcn_permlane32_swap((unsigned)k[0], (unsigned)k[NH - 1], false, false);
+    q4.s_hi = kE8M0One - (int)__builtin_amdgcn_permlane16_swap(half[0], half[1], false, false)[0];
+    q4.s_lo = q4.s_hi - 4;
+    q4.hi[0] = i32x8{(int)hw[0], (int)hw[1], (int)hw[2], (int)hw[3], (int)hw[4], (int)hw[5], (int)hw[6], (int)hw[7]};
+    q4.lo[0] = i32x8{(int)lw[0], (int)lw[1], (int)lw[2], (int)lw[3], (int)lw[4], (int)lw[5], (int)lw[6], (int)lw[7]};
+    if constexpr (D == 64) {
+        q4.hi[1] = i32x8{0, 0, 0, 0, (int)hw[0], (int)hw[1], (int)hw[2], (int)hw[3]};
+        q4.lo[1] = i32x8{0, 0, 0, 0, (int)lw[0], (int)lw[1], (int)lw[2], (int)lw[3]};
+    }
 }
 
 __device__ __forceinline__ f32x4 mfma_f4(const u32x4& a, int scale_a, const i32x8& b, int scale_b, f32x4 c) {

@@ -1099,9 +1099,9 @@ constexpr int kValuPerMfma = 7;
 // FP4 (4-bit pools): K tiles reach LDS as they lie, codes and scales, and are A
 // of v_mfma_scale_f32_32x32x64_f8f6f4 as e2m1 (lane (h, i): row i, k = 32 h ..
 // 32 h + 31, its scale), no widening.  B holds the query as e4m3 terms hi + lo,
-// scaled by a power of two a column (lane (h, c): k = 16 h + 0..15 and 32 + 16 h +
-// 0..15), exact for bf16 within 2^-14 of the row's largest: two products of 64
-// dims at twice bf16's rate.  Values come from the fp16 copy.  Widening the keys
+// scaled by a power of two a column and 32 dims (lane (h, c): k = 16 h + 0..15 and
+// 32 + 16 h + 0..15, and the scale of k = 32 h .. 32 h + 31), exact for bf16 within
+// 2^-14 of the block's largest: two products of 64 dims at twice bf16's rate.  Values come from the fp16 copy.  Widening the keys
 // to bf16 in LDS instead: eight chats' 16-256 new tokens after 2-8k 122 us, not
 // 112, four 2,048-token chunks after 4-10k 1049, not 996-1019 (whole calls).
 template <int D, int NH, bool FP8, bool FP4>
@@ -1208,40 +1208,47 @@ prefill_attn_kernel(PrefillArgs a) {
     const float sl = fabsf(s_eff);
     bf16x8 qv[FP4 ? 1 : D / 16];
     i32x8 q_hi[FP4 ? D / 64 : 1], q_lo[FP4 ? D / 64 : 1];
-    int qs_hi = 0, qs_lo = 0;
+    int qs[FP4 ? D / 64 : 1];      // scale bytes of product j: hi's, lo's
     if constexpr (FP4) {
-        // scaled so that the row's largest magnitude lies in [2^7, 2^8); the
-        // instruction's scales take that out, and lo's 2^4
+        // each 32-dim block scaled for itself, its largest magnitude into [2^7,
+        // 2^8); the instruction's scales take that out, and lo's 2^4.  The lane
+        // holds half of each block and gives the scale of block 2 j + hl.
         const uint32_t flip = s_eff < 0.f ? 0x80008000u : 0u;
         const uint16_t* qrow = a.q + (int64_t)(t0 + tok) * a.q_st + (int64_t)h * a.q_sh + 16 * hl;
-        u32x4 u[D / 16];
-        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            u[i] = *(const u32x4*)(qrow + 32 * (i >> 1) + 8 * (i & 1)) ^ flip;
+        for (int j = 0; j < D / 64; ++j) {
+            int k[2];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) m = max(m, max(u[i][k] & 0x7fffu, (u[i][k] >> 16) & 0x7fffu));
-        }
-        m = max(m, __float_as_uint(swap_halves(__uint_as_float(m))));
-        const int k = max(-120, min(134 - (int)(m >> 7), 120));
-        const float sq = __uint_as_float((uint32_t)(k + 127) << 23);
-        qs_hi = 127 - k;
-        qs_lo = 123 - k;
+            for (int e = 0; e < 2; ++e) {
+                u32x4 u[2];
+                uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j)
+                for (int i = 0; i < 2; ++i) {
+                    u[i] = *(const u32x4*)(qrow + 64 * j + 32 * e + 8 * i) ^ flip;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {          // four dims a dword
-                const u32x4 w4 = u[4 * j + (i >> 1)];
-                const uint32_t w0 = i & 1 ? w4.z : w4.x, w1 = i & 1 ? w4.w : w4.y;
-                const float v[4] = {__uint_as_float(w0 << 16) * sq, __uint_as_float(w0 & 0xffff0000u) * sq,
-                                    __uint_as_float(w1 << 16) * sq, __uint_as_float(w1 & 0xffff0000u) * sq};
-                int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-                c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
-                const f32x2 h01 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-                q_hi[j][i] = c;
-                c = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[0] - h01.x), 16.f * (v[1] - h01.y), 0, false);
-                q_lo[j][i] = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[2] - h23.x), 16.f * (v[3] - h23.y), c, true);
+                    for (int x = 0; x < 4; ++x) m = max(m, max(u[i][x] & 0x7fffu, (u[i][x] >> 16) & 0x7fffu));
+                }
+                m = max(m, __float_as_uint(swap_halves(__uint_as_float(m))));
+                k[e] = max(-120, min(134 - (int)(m >> 7), 120));
+                const float sq = __uint_as_float((uint32_t)(k[e] + 127) << 23);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {      // four dims a dword
+                    const u32x4 w4 = u[i >> 1];
+                    const uint32_t w0 = i & 1 ? w4.z : w4.x, w1 = i & 1 ? w4.w : w4.y;
+                    const float v[4] = {__uint_as_float(w0 << 16) * sq, __uint_as_float(w0 & 0xffff0000u) * sq,
+                                        __uint_as_float(w1 << 16) * sq, __uint_as_float(w1 & 0xffff0000u) * sq};
+                    int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+                    c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+                    const f32x2 h01 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+                    q_hi[j][4 * e + i] = c;
+                    c = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[0] - h01.x), 16.f * (v[1] - h01.y), 0, false);
+                    q_lo[j][4 * e + i] =
+                        __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (v[2] - h23.x), 16.f * (v[3] - h23.y), c, true);
+                }
             }
+            const int s_hi = 127 - (hl ? k[1] : k[0]);
+            qs[j] = s_hi | (s_hi - 4) << 8;
+        }
     } else {
         const uint32_t flip = s_eff < 0.f ? 0x80008000u : 0u;
         // the B operand of MFMA kb: dims 16 kb + 8 hl (fp8: 32 (kb / 2) + 16 hl + 8 (kb % 2))
@@ -1462,8 +1469,10 @@ prefill_attn_kernel(PrefillArgs a) {
 #pragma unroll
                     for (int hh = 0; hh < NH; ++hh) {
                         const i32x8 ka = {(int)kc[hh][j].x, (int)kc[hh][j].y, (int)kc[hh][j].z, (int)kc[hh][j].w, 0, 0, 0, 0};
-                        sc[hh] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                            ka, e ? q_lo[j] : q_hi[j], sc[hh], 4 /* e2m1 */, 0 /* e4m3 */, 0, ks[hh][j], 0, e ? qs_lo : qs_hi);
+                        sc[hh] = e ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                         ka, q_lo[j], sc[hh], 4 /* e2m1 */, 0 /* e4m3 */, 0, ks[hh][j], 1 /* byte */, qs[j])
+                                   : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q_hi[j], sc[hh], 4, 0, 0, ks[hh][j], 0,
+                                                                                     qs[j]);
                     }
         } else if constexpr (FP8) {
 #pragma unroll

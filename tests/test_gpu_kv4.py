@@ -799,3 +799,48 @@ def test_another_stream():
     kv4.write(*c.pools, kf, kf, c.table, c.lens, [1, 1])
     ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1, 1], 0.1)
     close(out, ref, mag, dot, DECODE)
+
+
+# ------------------------------------------- sizes within one query, one page --
+
+def lost_terms(qf, c, new, scale):
+    """[T, H_q, 1]: of each row the largest sum over 32-dim blocks of a query's
+    largest magnitude times the key's magnitudes, scaled.  A query dim below
+    2^-14 of its block's largest loses bits: it is held within 2^-21 of that."""
+    T, H_q, D = qf.shape
+    top = np.abs(qf).reshape(T, H_q, D // 32, 32).max(-1)
+    out, i = np.zeros((T, H_q, 1)), 0
+    for b, n in enumerate(new):
+        L = int(c.lens[b])
+        k = np.abs(kv4.read_pages(c.pools[0], c.table[b, :(L + 15) // 16], "k")[:L]).reshape(L, c.H, D // 32, 32).sum(-1)
+        for h in range(H_q):
+            out[i:i + n, h, 0] = (top[i:i + n, h] @ k[:, h // (H_q // c.H)].T).max(-1) * abs(scale)
+        i += n
+    return out
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("where", ["blocks", "dims"])
+def test_query_dims_of_very_different_sizes(D, where):
+    """Dims of 2^-30 to 1 in one query, whose small blocks meet keys as much
+    larger, or side by side in a block: every product counts."""
+    rng = np.random.default_rng(D)
+    H, G, new, scale = 2, 3, [1, 20, 1], D ** -0.5
+    lens = [200, 90, 700]
+    exps = np.stack([rng.permutation(np.linspace(0, 30, D // 32)).round() for _ in range(H)])       # [H, D / 32]
+
+    def fill(kind, b, i, shape):
+        x = rng.standard_normal(shape)
+        return x * np.repeat(np.exp2(exps), 32, -1)[:, None] if kind == "k" and where == "blocks" else x
+    c = Cache(rng, lens, H, D, fill=fill).to_device()
+    T = sum(new)
+    size = np.repeat(-exps, 32, -1).repeat(G, 0)[None] if where == "blocks" else rng.integers(-30, 1, (T, G * H, D))
+    qf, q = bf16(rng.standard_normal((T, G * H, D)) * np.exp2(size) * 2)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, new, scale)
+    lost = 2.0 ** -8 * lost_terms(qf, c, new, scale)             # 2^-20 of it, in close()'s 2^-12
+    out = torch.empty_like(q)
+    bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), scale, out)
+    close(out, ref, mag, dot + lost, PROMPT)
+    last = np.cumsum(new) - 1
+    for kw in ({}, dict(max_waves=1), dict(max_waves=7)):
+        close(decode(c, q[last].contiguous(), scale, **kw), ref[last], mag[last], (dot + lost)[last], DECODE, str(kw))
