@@ -415,8 +415,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * error budget).  Over bf16 pools the values the call reads are first copied
  * into the workspace as fp16, each 64-token step of a (request, KV head) at
  * the power of two 2^e that brings its largest magnitude M into
- * [2^14, 2^15): every value of at least M 2^-28 converts exactly, none
- * overflows; the output is kept at the finest step's scale, a coarser step's
+ * [2^14, 2^15): every value of at least M 2^-28 converts exactly, smaller ones
+ * keep an absolute error below M 2^-40, none overflows; the output is kept at the finest step's scale, a coarser step's
  * weights are multiplied by the difference, and 2^-e is taken out at the end
  * (values more than 2^63 below the largest of a key range lose bits).  Over fp8 pools the
  * codes are staged in LDS as bytes and widened exactly at the operand load
@@ -424,7 +424,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * V scale into the final normalisation.  Over 4-bit pools the keys enter the
  * matrix cores as they lie, against the query as two e4m3 terms (scores within
  * the decode attention's bound), and the values are copied to fp16 as over
- * bf16 pools; a page outside the pool makes the rows that see it NaN, a NaN
+ * bf16 pools (M the step's largest over all D dims, whatever their blocks'
+ * scales); a page outside the pool makes the rows that see it NaN, a NaN
  * key block the (request, head)'s rows that see its token, a NaN value block
  * its 32 dims of them.  Scratch
  * in the per-device

@@ -844,3 +844,43 @@ def test_query_dims_of_very_different_sizes(D, where):
     last = np.cumsum(new) - 1
     for kw in ({}, dict(max_waves=1), dict(max_waves=7)):
         close(decode(c, q[last].contiguous(), scale, **kw), ref[last], mag[last], (dot + lost)[last], DECODE, str(kw))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("spread", [8, 40, 100])
+@pytest.mark.parametrize("cached,new", [([200, 0, 47], [40, 100, 17]), ([2400, 700], [30, 1])], ids=["whole", "keys-shared-out"])
+def test_prompt_values_of_very_different_sizes(D, spread, cached, new):
+    """Scales from 2^-spread to 2^spread over tokens and blocks.  Beside the
+    roundings that close() knows: a value is held within 2^-40 of the largest of
+    its 64-token step (the fp16 copy), a weight within 2^-25 of the row's largest
+    (fp16), so A grows by 2^-40 / c of the weights times those largest values and
+    by 2^-25 / c of the values' sum."""
+    rng = np.random.default_rng(spread + D)
+    H, G, scale = 2, 3, 0.05
+
+    def fill(kind, b, i, shape):
+        x = rng.standard_normal(shape)
+        if kind == "v":
+            x = x * np.repeat(np.exp2(rng.integers(-spread, spread + 1, shape[:2] + (D // 32,))), 32, -1)
+        return x
+    c = Cache(rng, np.add(cached, new), H, D, fill=fill).to_device()
+    T = sum(new)
+    qf, q = bf16(rng.standard_normal((T, G * H, D)))
+    out = torch.empty_like(q)
+    bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), scale, out)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, new, scale)
+    i = 0
+    for b, n in enumerate(new):
+        L = int(c.lens[b])
+        pages = c.table[b, :(L + 15) // 16]
+        k, v = kv4.read_pages(c.pools[0], pages, "k")[:L], np.abs(kv4.read_pages(c.pools[1], pages, "v")[:L])
+        for h in range(G * H):
+            g = h // G
+            top = np.array([v[t // 64 * 64:t // 64 * 64 + 64, g].max() for t in range(L)])
+            seen = np.arange(L)[None, :] <= (L - n + np.arange(n))[:, None]
+            w = np.where(seen, np.exp(qf[i:i + n, h] @ k[:, g].T * scale), 0)
+            w /= w.sum(-1, keepdims=True)
+            mag[i:i + n, h] += (2.0 ** -40 * (w @ top)[:, None] + 2.0 ** -25 * (seen @ v[:, g])) / PROMPT
+        i += n
+    close(out, ref, mag, dot, PROMPT)
+    assert bl.device_errors() == 0
