@@ -132,6 +132,7 @@ typedef struct bellman_tensor {
  * Hence no two requests of one call may append into the same page.
  * A request whose slot lies outside the block table or the pool is skipped
  * (no byte written, length unchanged) and flagged in the device error word.
+ * B below 2^23.
  */
 int bellman_kv_append(const bellman_tensor_t *k_new, const bellman_tensor_t *v_new,
                       bellman_tensor_t *k_pages, bellman_tensor_t *v_pages,
@@ -325,8 +326,9 @@ int bellman_decode_step(const bellman_tensor_t *k_new, const bellman_tensor_t *v
  * holds two slots).  A token outside its
  * request's table or the pool is skipped and flagged (flag 1), and that
  * request's length is left unchanged when its last position does not fit.
- * Once the workspace has grown to the call's size, the call enqueues only
- * kernels on `stream` (graph-capturable). */
+ * T / 16 + 2 B + 1 (pages, at most) below 2^24.  Once the workspace has grown
+ * to the call's size, the call enqueues only kernels on `stream`
+ * (graph-capturable). */
 int bellman_kv_write(const bellman_tensor_t *k_new, const bellman_tensor_t *v_new,
                      bellman_tensor_t *k_pages, bellman_tensor_t *v_pages,
                      const bellman_tensor_t *block_table, bellman_tensor_t *seq_lens,
@@ -345,8 +347,8 @@ int bellman_kv_write(const bellman_tensor_t *k_new, const bellman_tensor_t *v_ne
  * pool reads as NaN (flag 4); rows of a malformed request (n_b < 0, n_b > L_b,
  * rows past T, L_b past the table) are not written (flag 2), and a q_start
  * that decreases, starts below 0 or ends past T reads no row at all, and rows
- * from q_start[B] on are left as they are (flag 2 in each case).  Workspace
- * and graph capture as for bellman_kv_write. */
+ * from q_start[B] on are left as they are (flag 2 in each case).  Limits,
+ * workspace and graph capture as for bellman_kv_write. */
 int bellman_kv_read(const bellman_tensor_t *k_pages, const bellman_tensor_t *v_pages,
                     const bellman_tensor_t *block_table, const bellman_tensor_t *seq_lens,
                     const bellman_tensor_t *q_start, bellman_tensor_t *k_out,
@@ -373,7 +375,7 @@ int bellman_kv_read(const bellman_tensor_t *k_pages, const bellman_tensor_t *v_p
  *   q_out, k_out  bf16, shaped as q and k (written, rounded to nearest even):
  *                 q and k themselves, or memory that overlaps no input.
  * Angles are formed in binary64, everything else in binary32 (a normed row whose
- * squares sum past its range gives zeros).  T below 2^26.  Enqueues one
+ * squares sum past its range gives zeros).  T at most 2^26 - 4.  Enqueues one
  * kernel, needs no workspace (graph-capturable).  opts NULL: eps 1e-6, no
  * offset, one axis, pairs (f, f + F). */
 typedef struct bellman_rope_opts {
@@ -406,6 +408,7 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  *                a malformed request (n_b > L_b, rows past T, L_b past the
  *                table: flag 2) are not written; a q_start that decreases, starts below
  *                0 or ends past T writes no row at all (flag 2).
+ * (T G / 128 + B) H_kv below 2^24 - 7.
  * Each workgroup takes 128 (token, query head) rows of one request and KV
  * head over all of their keys, or over a share of them where the rows would
  * leave the device idle (merged in fp32 by a second pass).  QK^T runs on the

@@ -301,6 +301,9 @@ int check_rows(const bellman_tensor_t* t, const char* name, int32_t dtype, int64
     return BELLMAN_OK;
 }
 
+// A launch holds fewer than 2^32 threads: workgroups of 256 up to this many.
+constexpr int64_t kMaxGroups256 = (INT64_C(1) << 24) - 1;
+
 int launch_status(const char* what) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(BELLMAN_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
@@ -624,11 +627,12 @@ int bellman_kv_append(const bellman_tensor_t* k_new, const bellman_tensor_t* v_n
     const int32_t row_dtype = quant || ps.fp4 ? (int32_t)BELLMAN_BF16 : k_pages->dtype;
     if ((rc = check_rows(k_new, "k_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
     if ((rc = check_rows(v_new, "v_new", row_dtype, B, ps.H_kv, ps.D, 16))) return rc;
+    // (a workgroup of 256 or 512 threads a request)
+    if (B > kMaxGroups256 / 2) return fail(BELLMAN_ERR_UNSUPPORTED, "2^23 requests or more");
     if ((rc = check_block_table(block_table, B))) return rc;
     if ((rc = check_seq_lens(seq_lens, B))) return rc;
     if (quant && (!k_pages->dequant_scale || !v_pages->dequant_scale))
         return fail(BELLMAN_ERR_INVALID_ARG, "quantising bf16 rows into fp8 pools needs dequant_scale on both pools");
-    if (B > INT32_MAX) return fail(BELLMAN_ERR_UNSUPPORTED, "batch too large");
     if (B == 0) return BELLMAN_OK;
 
     int dev;
@@ -761,12 +765,12 @@ static int write_or_read(bool read, const bellman_tensor_t* k_new, const bellman
     if ((rc = check_rows(v_new, vname, row_dtype, T, ps.H_kv, ps.D, 16))) return rc;
     if ((rc = check_seq_lens(seq_lens, seq_lens ? seq_lens->shape[0] : 0))) return rc;
     const int64_t B = seq_lens->shape[0];
+    // (a workgroup a page: at most T / 16 + 2 B + 1 of them)
+    if (T > INT32_MAX || B > INT32_MAX || T / kPage + 2 * B + 1 > kMaxGroups256)
+        return fail(BELLMAN_ERR_UNSUPPORTED, "too many tokens or requests: T / 16 + 2 B + 1 must stay below 2^24");
     if ((rc = check_block_table(block_table, B))) return rc;
     if ((rc = check_q_start(q_start, B))) return rc;
-    if (T > INT32_MAX || B > INT32_MAX) return fail(BELLMAN_ERR_UNSUPPORTED, "too many tokens or requests");
     if (T == 0 || B == 0) return BELLMAN_OK;
-
-    if (T / 16 + 2 * B + 1 > (int64_t)UINT32_MAX) return fail(BELLMAN_ERR_UNSUPPORTED, "too many tokens or requests");
 
     int dev;
     if ((rc = current_device(&dev))) return rc;
@@ -875,8 +879,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t* q, const bellman_tensor_t* k, c
     if (!aligned(positions->data, 4)) return fail(BELLMAN_ERR_UNSUPPORTED, "positions: misaligned data");
     if (H_q < 1 || H_kv < 1) return fail(BELLMAN_ERR_INVALID_ARG, "q and k need a head each");
     if (H_q > 65535 || H_kv > 65535) return fail(BELLMAN_ERR_UNSUPPORTED, "more than 65535 heads");
-    // (a token takes a wave; a launch holds fewer than 2^32 threads)
-    if (T >= INT64_C(1) << 26) return fail(BELLMAN_ERR_UNSUPPORTED, "2^26 tokens or more");
+    // (a token takes a wave, four a workgroup)
+    if ((T + 3) / 4 > kMaxGroups256) return fail(BELLMAN_ERR_UNSUPPORTED, "2^26 tokens or more (a launch holds 2^26 - 4)");
     RopeArgs a;
     // axis x turns sections[x] frequencies, in order
     int64_t sum = 0;
@@ -939,7 +943,6 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     if ((rc = check_seq_lens(seq_lens, seq_lens ? seq_lens->shape[0] : 0))) return rc;
     const int64_t B = seq_lens->shape[0];
     if ((rc = check_block_table(block_table, B))) return rc;
-    if ((rc = check_q_start(q_start, B))) return rc;
     if (!isfinite(scale)) return fail(BELLMAN_ERR_INVALID_ARG, "scale must be finite");
     if (H_q < 1 || H_q % ps.H_kv != 0)
         return fail(BELLMAN_ERR_INVALID_ARG, "query heads %lld not a multiple of KV heads %d", (long long)H_q, ps.H_kv);
@@ -948,6 +951,10 @@ int bellman_prefill_attention_opts(const bellman_tensor_t* q, const bellman_tens
     // tiles x query heads must fit the kernel's 32-bit work index
     if (((T + kPrefillRows - 1) / kPrefillRows + B) * H_q > INT32_MAX / 2)
         return fail(BELLMAN_ERR_UNSUPPORTED, "too many query tiles x heads");
+    // (a workgroup a tile and KV head, in eights)
+    if ((T * (H_q / ps.H_kv) / kPrefillRows + B) * ps.H_kv > kMaxGroups256 - 7)
+        return fail(BELLMAN_ERR_UNSUPPORTED, "too many query tiles x KV heads: (T G / 128 + B) H_kv must stay below 2^24 - 7");
+    if ((rc = check_q_start(q_start, B))) return rc;
     if (T == 0 || B == 0) return BELLMAN_OK;
 
     // bf16 and 4-bit pools: the fp16 copy of the values holds at most every table page

@@ -294,3 +294,37 @@ def test_native_forms_hand_over_the_same_descriptors(form, tensors, opts, option
         assert B._native(addr, n, 0, 0.0, 0, None, None, *ts) is None
     with pytest.raises(TypeError):
         B._native(addr, n, 0, 0.0, 0, None, None, *([host] * (tensors - 1)))
+
+
+def wide4(Bsz, T):
+    """Descriptors whose sizes a launch just holds, or just does not; the last
+    argument checked after the sizes is wrong, so no call gets past the checks."""
+    g = good4(Bsz=Bsz, D=64, Hq=1, H=1, T=T)
+    g.update(qs=t(B.INT32, [Bsz + 2]), sl=t(B.INT32, [Bsz]), bt=t(B.INT32, [Bsz, 1]))
+    return g
+
+
+@pytest.mark.parametrize("call,held,refused,later,text", [
+    # workgroups of 256 (append: 512 over other pools) threads, fewer than 2^32 in all
+    ("append", ((1 << 23) - 1, 1), (1 << 23, 1), "seq_lens", "2^23 requests"),
+    ("write", (1, (1 << 28) - 49), (1, (1 << 28) - 48), "q_start", "tokens or requests"),
+    ("write", ((1 << 23) - 2, 47), ((1 << 23) - 2, 48), "q_start", "tokens or requests"),
+    ("read", (1, (1 << 28) - 49), (1, (1 << 28) - 48), "q_start", "tokens or requests"),
+    ("prefill", (1, ((1 << 24) - 9) * 128 + 127), (1, ((1 << 24) - 9) * 128 + 128), "q_start", "KV heads"),
+])
+def test_sizes_that_a_launch_does_not_hold(call, held, refused, later, text):
+    L = B.library()
+    for size, word in ((held, later), (refused, text)):
+        g = wide4(*size)
+        if call == "append":
+            g["sl"] = t(B.INT32, [size[0] + 1])
+        if call == "prefill":       # (2^30 tokens and more are refused before: a wider group has as many rows)
+            g.update(qt=t(B.BF16, [size[1] // 16, 16, 64]), ot=t(B.BF16, [size[1] // 16, 16, 64]))
+        assert CALLS[call](L, g) in (ERR_INVALID, ERR_UNSUPPORTED)
+        assert word in B.last_error(), B.last_error()
+
+
+def test_rope_tokens_that_a_launch_does_not_hold():
+    for T, text in (((1 << 26) - 4, "sections sum"), ((1 << 26) - 3, "2^26 tokens"), ((1 << 26) - 1, "2^26 tokens")):
+        a = {**rope_args(T=T), "o": sect(32, 30), "pos": t(B.INT32, [2, T])}
+        assert call_rope(a) in (ERR_INVALID, ERR_UNSUPPORTED) and text in B.last_error(), B.last_error()
