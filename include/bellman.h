@@ -225,10 +225,10 @@ typedef struct bellman_attn_opts {
                              starts, [3w+1] = the clock when it has written its
                              last result, [3w+2] = (XCD id << 32) | HW_ID of its
                              SIMD.  A timing record: the results are those of the
-                             untraced call.  Built for head_dim 128 at the default
-                             steps (bf16: pages_per_step 1 or 2 with
-                             pipeline_depth 0 or 2; fp8: 4 pages, depth 1); other
-                             shapes return BELLMAN_ERR_UNSUPPORTED.  NULL = none */
+                             untraced call.  Built for bf16 and fp8 pools of
+                             head_dim 128 at the default steps (bf16:
+                             pages_per_step 1 or 2 with pipeline_depth 0 or 2;
+                             fp8: 4 pages, depth 1); other shapes return BELLMAN_ERR_UNSUPPORTED.  NULL = none */
 } bellman_attn_opts_t;
 
 /* bellman_decode_attention with explicit tuning options (NULL = defaults).

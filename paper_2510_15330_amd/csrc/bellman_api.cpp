@@ -367,6 +367,8 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     if (ps.fp4 && pps != 0 && pps != 4)
         return fail(BELLMAN_ERR_UNSUPPORTED, "pages_per_step %d: 4-bit pools take 4 pages a step", pps);
     if (ps.fp4 && depth == 2) return fail(BELLMAN_ERR_UNSUPPORTED, "pipeline_depth 2 is not built for 4-bit pools");
+    if (ps.fp4 && opts && opts->wave_times)
+        return fail(BELLMAN_ERR_UNSUPPORTED, "wave_times: no traced kernel is built for 4-bit pools");
     const bool chosen = pps == 0 && depth == 0;   // the step is the library's choice
     if (depth == 0) depth = ps.kv == kKvBf16 ? 2 : 1;
     if (B == 0) return BELLMAN_OK;

@@ -328,3 +328,12 @@ def test_rope_tokens_that_a_launch_does_not_hold():
     for T, text in (((1 << 26) - 4, "sections sum"), ((1 << 26) - 3, "2^26 tokens"), ((1 << 26) - 1, "2^26 tokens")):
         a = {**rope_args(T=T), "o": sect(32, 30), "pos": t(B.INT32, [2, T])}
         assert call_rope(a) in (ERR_INVALID, ERR_UNSUPPORTED) and text in B.last_error(), B.last_error()
+
+
+@pytest.mark.parametrize("call", ["decode", "step"])
+def test_no_traced_kernel_over_4_bit_pools(call):
+    for change in ({}, dict(q=t(B.BF16, [4, 32, 64]), out=t(B.BF16, [4, 32, 64]), kn=t(B.BF16, [4, 8, 64]),
+                            vn=t(B.BF16, [4, 8, 64]), k=t(B.FP4_E2M1, [100, 8, 17, 32]), v=t(B.FP4_E2M1, [100, 8, 17, 32]))):
+        g = {**good4(), **change, "opts": opts(wave_times=FAKE)}
+        assert CALLS[call](B.library(), g) == ERR_UNSUPPORTED
+        assert "4-bit pools" in B.last_error(), B.last_error()
