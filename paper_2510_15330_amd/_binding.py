@@ -217,8 +217,9 @@ _DTYPES = {
     torch.float8_e4m3fn: FP8_E4M3FN,
     torch.int32: INT32,
     torch.float32: FP32,
-    torch.float4_e2m1fn_x2: FP4_E2M1,  # 4-bit pools: bytes of two codes, and scale bytes
 }
+if hasattr(torch, "float4_e2m1fn_x2"):     # (a torch without it has the other pools)
+    _DTYPES[torch.float4_e2m1fn_x2] = FP4_E2M1   # 4-bit pools: bytes of two codes, and scale bytes
 
 
 def desc(t: torch.Tensor, dequant_scale: torch.Tensor | None = None) -> Tensor:

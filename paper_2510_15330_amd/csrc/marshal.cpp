@@ -16,7 +16,8 @@
 namespace {
 
 PyObject *g_tensor, *g_parameter;             // the exact types taken
-constexpr int kDtypes = 6;
+constexpr int kDtypes = 6;                    // at most
+int g_dtypes;
 PyObject* g_dtype[kDtypes];                   // torch dtypes, and their codes
 int32_t g_code[kDtypes];
 PyObject *g_raw_stream, *g_device;            // current stream of a device, current device
@@ -50,7 +51,7 @@ bool device_tensor(PyObject* t) {
 
 int dtype_index(PyObject* t) {
     Ref r(PyObject_GetAttr(t, s_dtype));
-    for (int i = 0; i < kDtypes; ++i)
+    for (int i = 0; i < g_dtypes; ++i)
         if (r.p == g_dtype[i]) return i;
     return -1;
 }
@@ -182,15 +183,17 @@ PyObject* call(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
-// setup(Tensor, Parameter, ((dtype, code), ...6), float32, raw_stream, device)
+// setup(Tensor, Parameter, ((dtype, code), ... up to 6), float32, raw_stream, device)
 PyObject* setup(PyObject*, PyObject* args) {
     PyObject *tensor, *parameter, *dtypes, *f32, *raw, *dev;
     if (!PyArg_ParseTuple(args, "OOO!OOO", &tensor, &parameter, &PyTuple_Type, &dtypes, &f32, &raw, &dev)) return nullptr;
-    if (PyTuple_GET_SIZE(dtypes) != kDtypes) {
-        PyErr_SetString(PyExc_ValueError, "setup: six element types");
+    const int n = (int)PyTuple_GET_SIZE(dtypes);
+    if (n > kDtypes) {
+        PyErr_SetString(PyExc_ValueError, "setup: more than six element types");
         return nullptr;
     }
-    for (int i = 0; i < kDtypes; ++i) {
+    g_dtypes = 0;
+    for (int i = 0; i < n; ++i) {
         PyObject* dt;
         int code;
         if (!PyArg_ParseTuple(PyTuple_GET_ITEM(dtypes, i), "Oi", &dt, &code)) return nullptr;
@@ -200,6 +203,7 @@ PyObject* setup(PyObject*, PyObject* args) {
         g_code[i] = code;
         if (dt == f32) g_float32 = i;
     }
+    g_dtypes = n;
     PyObject** const slots[] = {&g_tensor, &g_parameter, &g_raw_stream, &g_device};
     PyObject* const vals[] = {tensor, parameter, raw, dev};
     for (int i = 0; i < 4; ++i) {

@@ -121,3 +121,24 @@ def test_descriptors_equal_the_ctypes_ones(form):
     assert B._native(addr, form, 0, 0.1, 0, None, None, *ok[:-1], torch.zeros(2, device=dev, dtype=torch.float64)) is None
     assert B._native(addr, form, 0, 0.1, 0, None, None, *ok[:-1], torch.zeros((1,) * 6, device=dev)) is None
     assert not seen
+
+
+def test_a_torch_without_the_4_bit_type():
+    # the package, its other pools and the native marshalling are there all the same
+    code = """
+import torch
+del torch.float4_e2m1fn_x2
+import paper_2510_15330_amd as bl
+from paper_2510_15330_amd import _binding as B
+assert bl.version() and B._native is not None
+assert B.desc(torch.zeros(2, 3, dtype=torch.bfloat16)).dtype == B.BF16
+try:
+    B.desc(torch.zeros(2, 3, dtype=torch.int64))
+except TypeError:
+    pass
+else:
+    raise AssertionError("accepted")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
