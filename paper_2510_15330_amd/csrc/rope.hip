@@ -4,7 +4,7 @@
 //
 // Bound by memory: (H_q + H_kv) D values a token read and written once (36,001
 // tokens of 32/8 heads of 128, 737 MB, in 128 us, 5.8 TB/s; 4,613 of 28/4 in
-// 15.8 us; 64 tokens 4.1 us, a launch's latency).  Six waves a SIMD (68
+// 15.8 us; 64 tokens 4.1 us, a launch's latency).  Six waves a SIMD (70
 // registers; at four, 8,000 tokens of 64 dims took 23 us instead of 17.4, and
 // loads a pass ahead cost more registers than they hid).  A row
 // is D / 16 lanes, each with two 16-byte units whose values pair up (dims i and
@@ -56,6 +56,8 @@ __device__ __forceinline__ float row_sum(float v) {
         v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));   // half mirror
     return v;
 }
+
+constexpr float kTinyMean = 0x1p-100f;   // from it on the squares that count are normal numbers
 
 // STREAM: the stores (1) or loads and stores (2) pass the caches by.
 template <int D, bool INTER, int STREAM>
@@ -131,7 +133,20 @@ __global__ void __launch_bounds__(256, 6) qk_norm_rope_kernel(RopeArgs a) {
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
-            const float inv = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + a.eps);
+            float ms = row_sum<LPR>(ss) * (1.f / D) + a.eps;
+            if (__any(ms < kTinyMean)) {
+                // rows of tiny values under a tiny eps: their squares leave
+                // binary32, so they are taken 2^75 times as large
+                const float up = ms < kTinyMean ? 0x1p75f : 1.f;
+                ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] *= up;
+                    ss = __builtin_fmaf(x[i], x[i], ss);
+                }
+                ms = row_sum<LPR>(ss) * (1.f / D) + a.eps * up * up;
+            }
+            const float inv = rsqrtf(ms);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = x[i] * inv * w[i];
         }

@@ -165,3 +165,15 @@ def test_nan_and_zero_rows_stay_their_own():
     # without a norm only the NaN's pair is
     bl.qk_norm_rope(x, x, pos, torch.logspace(0, -3, 32, device="cuda"), a, b)
     assert torch.isnan(a).sum() == 2 and torch.isnan(a[2, 1, [5, 37]]).all()
+
+
+@pytest.mark.parametrize("D,inter", [(64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("scale", [1e-20, 2.0 ** -54, 2.0 ** -66, 2.0 ** -100, 2.0 ** -128])
+def test_rows_whose_squares_are_below_binary32(D, inter, scale):
+    """With an eps of the rows' own size or none; other rows of the call as ever."""
+    rng = np.random.default_rng(D)
+    for eps in (0.0, 1e-40, 1e-32):
+        run(rng, 9, 4, 2, D, D // 2, rng.integers(0, 99, 9), qw=torch.float32, kw=torch.bfloat16, eps=eps, scale=scale, inter=inter)
+        mixed = np.exp2(rng.integers(-130, 10, (9, 4 + 2 + 2, 1))).astype(np.float32)
+        run(rng, 9, 4, 2, D, D // 2, rng.integers(0, 99, 9), qw=torch.float32, kw=torch.bfloat16, eps=eps, scale=torch.from_numpy(mixed),
+            inter=inter)
