@@ -884,3 +884,80 @@ def test_prompt_values_of_very_different_sizes(D, spread, cached, new):
         i += n
     close(out, ref, mag, dot, PROMPT)
     assert bl.device_errors() == 0
+
+
+# ------------------------------------------------------- errors as a whole --
+
+def noise(qf, c, new, scale):
+    """(out, spread, dot): spread the root of the sum of squares of a row's
+    weights times values, what independent relative errors of its weights add up
+    to; dot the largest sum of |products| of a score."""
+    T, H_q, D = qf.shape
+    out, spread, dot, i = np.zeros(qf.shape), np.zeros(qf.shape), np.zeros((T, H_q, 1)), 0
+    for b, n in enumerate(new):
+        L = int(c.lens[b])
+        pages = c.table[b, :(L + 15) // 16]
+        k, v = (kv4.read_pages(p, pages, kind)[:L] for p, kind in zip(c.pools, "kv"))
+        seen = np.arange(L)[None, :] <= (L - n + np.arange(n))[:, None]
+        for h in range(H_q):
+            g = h // (H_q // c.H)
+            s = np.where(seen, qf[i:i + n, h] @ k[:, g].T * scale, -np.inf)
+            w = np.exp(s - s.max(-1, keepdims=True))
+            w /= w.sum(-1, keepdims=True)
+            out[i:i + n, h] = w @ v[:, g]
+            spread[i:i + n, h] = np.sqrt(w ** 2 @ v[:, g] ** 2)
+            dot[i:i + n, h, 0] = (np.abs(qf[i:i + n, h]) @ np.abs(k[:, g]).T).max(-1) * abs(scale)
+        i += n
+    return out, spread, dot
+
+
+def close_as_a_whole(got, qf, c, new, scale, weight, what=""):
+    """The norm of the errors of a call's outputs.  A rounding to bf16 is spread
+    over +-2^-8 / (1 .. 2) of the value, rms at most 2^-8 / sqrt(3) of it; a
+    weight is off by `weight` and by its score's error, 2^-13 dot at most, from
+    key to key independently."""
+    ref, spread, dot = noise(qf, c, new, scale)
+    got = got.float().cpu().double().numpy()
+    bound = 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(ref) + np.linalg.norm((weight + 2.0 ** -13 * dot) * spread)
+    off = np.linalg.norm(got - ref)
+    assert off <= bound, f"{what}: {off / np.linalg.norm(ref):.3e} of the outputs, {bound / np.linalg.norm(ref):.3e} allowed"
+
+
+@pytest.mark.parametrize("D,H,G", [(64, 2, 4), (128, 2, 4), (128, 1, 16), (64, 3, 1)])
+@pytest.mark.parametrize("lens", [[50, 200, 7], [9000, 4000]], ids=["short", "long"])
+def test_errors_as_a_whole(D, H, G, lens):
+    rng = np.random.default_rng(D + H + G)
+    scale = D ** -0.5
+    c = Cache(rng, lens, H, D).to_device()
+    qf, q = bf16(rng.standard_normal((len(lens), G * H, D)))
+    for kw in ({}, dict(max_waves=1), dict(max_waves=100)):
+        close_as_a_whole(decode(c, q, scale, **kw), qf, c, [1] * len(lens), scale, 2.0 ** -14, f"decode {kw}")
+    new = [min(30, n) for n in lens]
+    qf, q = bf16(rng.standard_normal((sum(new), G * H, D)))
+    out = torch.empty_like(q)
+    bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), scale, out)
+    close_as_a_whole(out, qf, c, new, scale, 2.0 ** -12, "prompt")
+
+
+@pytest.mark.parametrize("H,waves", [(4, (8, 12, 16)), (2, (6, 8)), (6, (10, 16, 24))])
+def test_weighted_shares_of_heads_side_by_side(H, waves):
+    """384 pages a wave and more, over workgroups of both weights: the waves that
+    take a group's heads side by side share one range of uneven size."""
+    rng = np.random.default_rng(H)
+    D, scale = 64, 0.125
+    lens = [11000, 1, 6500, 0, 8200]
+    c = Cache(rng, lens, H, D).to_device()
+    qf, q = bf16(rng.standard_normal((5, 2 * H, D)))
+    keep = [b for b, n in enumerate(lens) if n]
+    pages = H * sum((n + 15) // 16 for n in lens)
+    ref, mag, dot = kv4.attention(qf, *c.pools, c.table, c.lens, [1] * 5, scale)
+    for w in waves:
+        assert pages >= 384 * w and w > 5
+        for skew in (255, 0, 100, -1):
+            out = decode(c, q, scale, max_waves=w, xcd_skew=skew)
+            close(out, ref, mag, dot, DECODE, f"{w} waves, skew {skew}")
+            assert not out[3].any() and torch.equal(out, decode(c, q, scale, max_waves=w, xcd_skew=skew))
+    sub = Cache.__new__(Cache)
+    sub.H, sub.pools, sub.table, sub.lens = c.H, c.pools, c.table[keep], c.lens[keep]
+    close_as_a_whole(out[keep], qf[keep], sub, [1] * len(keep), scale, 2.0 ** -14)
+    assert bl.device_errors() == 0
