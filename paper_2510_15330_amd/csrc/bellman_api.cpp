@@ -442,13 +442,20 @@ int decode_attention(const bellman_tensor_t* q, const bellman_tensor_t* k_pages,
     // 0.5-8k, 77 table pages a wave, 26.9 / 26.2, 28 of them, 108 pages, 31.2 /
     // 31.4 at 4 heads and 34.6 / 32.4 at 8).
     // Over 4-bit pools a step is half an fp8 step's bytes and as many
-    // instructions, and the second workgroup pays from shorter shares on (two /
-    // one, table pages a wave of one in brackets): at head_dim 128 and 4 heads, 256
-    // requests of 6-13.5k [1690] 448 / 474 us, 400 of 3-5k [980] 299 / 308, 100 of
-    // 4-8k [390] 116.7 / 121.1, 128 of 2-6k [375] 104.5 / 103.7, 64 of 1-4k [128]
-    // 42.6 / 41.6, at 16 heads 256 of 6-13.5k on one KV head 81.5 / 77.9; at
-    // head_dim 64, 300 of 2-8k [1170] 175 / 230, 64 of 1-4k [128] 28.4 / 33.4, 40
-    // of them [80] 23.6 / 24.1, 20 of 0.5-8k [78] 25.5 / 22.8.
+    // instructions, and the second workgroup pays from shorter shares on, the
+    // later the more heads there are.  Two / one, us, by query heads a KV head
+    // (8 KV heads; table pages a wave of one in brackets), at head_dim 128
+    //   256 of 6-13.5k [1686]  1: 435 / 472    4: 447 / 478    8: 465 / 482    16: 524 / 507
+    //   400 of 3-5k    [978]      287 / 311       301 / 315       323 / 322        372 / 352
+    //   100 of 4-8k    [384]      110 / 113       115 / 117       124 / 119        146 / 140
+    //   128 of 2-6k    [366]     97.5 / 99.2      105 / 101       114 / 109        134 / 126
+    //   64 of 1-4k     [125]     38.9 / 39.8     42.8 / 41.8     48.8 / 45.2      55.8 / 52.3
+    // and at head_dim 64
+    //   300 of 2-8k    [1170]     177 / 227       175 / 230       184 / 231        198 / 234
+    //   64 of 1-4k     [125]     27.7 / 32.8     28.4 / 33.4     31.0 / 34.9      35.9 / 36.4
+    //   40 of 1-4k     [77]      23.0 / 23.6     23.6 / 24.1     26.8 / 25.6      30.9 / 27.5
+    //   20 of 0.5-8k   [74]      24.4 / 22.6     25.5 / 22.8     29.9 / 25.2      37.0 / 28.3
+    // (within 5% of the better one throughout).
     bool two = chosen && ps.fp8 &&
                (ps.D == 64 ? table_pages_per_wave >= std::max(96.0, 14.0 * (double)G)
                            : G <= 8 && table_pages_per_wave >= kWideTablePages);

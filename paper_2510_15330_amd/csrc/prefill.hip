@@ -584,7 +584,11 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(WriteArgs a, const int32_
 }
 
 // bf16 pools (copies) and fp8 pools (code times the (request, head)'s scale,
-// rounded to nearest even).
+// rounded to nearest even).  K units go straight to their rows, V's dim-major
+// ones through LDS.  Bound by memory: 37,461 tokens of 8 heads of 128, bf16 307 MB
+// in 58.6 us (5.2 TB/s), fp8 230 MB in 39.5 (5.8); of 64, fp8 115 MB in 25.4
+// (4.5: a quarter of the threads has a unit); 1,047 tokens 5.2 us, a launch and a
+// chain of three loads.
 template <int EB>
 __global__ void __launch_bounds__(256) kv_read_kernel(WriteArgs a, const int32_t* page_start) {
     __shared__ __attribute__((aligned(16))) uint16_t vst[kPage * (128 + 8)];

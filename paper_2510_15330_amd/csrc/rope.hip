@@ -12,8 +12,9 @@
 // wave walks a token's rows, 64 / (D / 16) at a time, queries first.  A lane's
 // eight angles are the same for all rows of the token: they are formed once a
 // wave, in turns, the product in binary64 (a position of 2^20 times a frequency
-// near 1 is exact to 2^-29 turns there, to 2^-3 in binary32), its fraction to
-// the sine and cosine units, which take turns (measured within 1.3e-7).
+// near 1 is within 2^-35 turns there, in binary32 2^-5.7), its fraction, rounded
+// to binary32 (2^-26), to the sine and cosine units, which take turns (measured
+// within 1.3e-7).
 // Everything between the loads and the rounding to bf16 is binary32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
