@@ -978,9 +978,10 @@ __global__ void __launch_bounds__(256) v4copy_kernel(PrefillArgs a) {
             L = a.seq_lens[b];
         }
         const int pi = (kPrefillKeys / kPage) * j + w;
-        const int nv = max(min(L - kPage * pi, kPage), 0);        // live slots of this wave's page
-        const int pg = nv > 0 ? a.block_table[(int64_t)b * a.bt_stride + pi] : 0;
+        const bool inside = kPage * pi < L;
+        const int pg = inside ? a.block_table[(int64_t)b * a.bt_stride + pi] : -1;
         const bool ok = (unsigned)pg < (unsigned)a.num_pages;
+        const int nv = ok ? min(L - kPage * pi, kPage) : 0;         // slots of this wave's page to copy
         const char* vp = (const char*)a.v_pages + ((int64_t)(ok ? pg : 0) * a.H_kv + g) * TB;
         const VT vc = *(const VT*)(vp + lane * (D / 8));
         const VT vs = *(const VT*)(vp + 8 * D + qg * (D / 8));

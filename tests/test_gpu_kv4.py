@@ -961,3 +961,32 @@ def test_weighted_shares_of_heads_side_by_side(H, waves):
     sub.H, sub.pools, sub.table, sub.lens = c.H, c.pools, c.table[keep], c.lens[keep]
     close_as_a_whole(out[keep], qf[keep], sub, [1] * len(keep), scale, 2.0 ** -14)
     assert bl.device_errors() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale_byte", [227, 254, 255])
+def test_a_page_outside_the_pool_takes_nothing_from_the_first(D, scale_byte):
+    """Rows before its tokens are those of the pages they see, whatever the
+    pool's first page holds: values of 2^100 and more, infinite ones, NaN."""
+    rng = np.random.default_rng(D)
+    H, lens = 2, [64, 70]
+    c = Cache(rng, lens, H, D, spare=40)
+    free = 0                                              # the first page, of no request
+    if free in c.table:
+        at, other = c.table == free, c.spare[0]
+        for pool in c.pools:
+            pool[other] = pool[free]
+        c.table[at] = other
+    for pool in c.pools:
+        pool[free, :, 16], pool[free, :, :16] = scale_byte, 0x77
+    c.table[0, 1] = c.pools[0].shape[0]
+    c.table[1, 4] = -1
+    c.to_device()
+    qf, q = bf16(rng.standard_normal((sum(lens), 4, D)))
+    out = torch.empty_like(q)
+    bl.prefill_attention(q, c.k, c.v, c.bt, c.sl, dev(np.array([0, 64, 134], dtype=np.int32)), 0.1, out)
+    assert bl.device_errors() == 4
+    for b, first, n in ((0, 0, 16), (1, 64, 64)):         # each request's rows before the page
+        ref, mag, dot = kv4.attention(qf[first:first + n], *c.pools, c.table[b:b + 1], np.array([n], dtype=np.int32), [n], 0.1)
+        close(out[first:first + n], ref, mag, dot, PROMPT, f"request {b}")
+    assert torch.isnan(out[16:64]).all() and torch.isnan(out[128:]).all()
