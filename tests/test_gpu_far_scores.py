@@ -1,4 +1,4 @@
-"""Prompt attention on finite scores of any size, over every kind of pool.
+"""Prompt and decode attention on finite scores of any size, over every kind of pool.
 
 Two tokens of a request hold the same key, along the query's signs and six
 times as long as the others': from queries of 2^14 on, every row is the mean of
@@ -8,7 +8,7 @@ by 2^3 (their copies have scales that differ).
 
 |got - ref| <= 2^-8 |ref| + (2^-11 + 2^-12 S) A against binary64 over the values
 that the pool holds, A the weighted sum of |values|: the output's rounding to
-bf16, the weights' to fp16 and the exponents' roundings; S, the sum of |products|
+bf16, the weights' to fp16 (decode: less) and the exponents' roundings; S, the sum of |products|
 of a row's largest score, counts below 2^14 alone, where weights depend on the
 scores' own error (2^-13 S over 4-bit pools, less over the others).
 """
@@ -46,9 +46,10 @@ def pools(kv, pages, D):
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8", "fp4"])
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("call", ["prompt", "decode"])
 @pytest.mark.parametrize("shift", [0, -110, 50])      # queries 2^shift, the softmax scale 2^-shift times as large
 @pytest.mark.parametrize("L,twins", [(340, (70, 200)), (2540, (100, 1700))], ids=["whole", "keys-shared-out"])
-def test_finite_scores_of_any_size(kv, D, L, twins, shift):
+def test_finite_scores_of_any_size(kv, D, L, twins, shift, call):
     rng = np.random.default_rng(D + L)
     n, G, scale = 40, len(POWERS), 0.1 * 2.0 ** -shift
     u = rng.choice([-1.0, 1.0], D)
@@ -70,9 +71,17 @@ def test_finite_scores_of_any_size(kv, D, L, twins, shift):
 
     q = torch.from_numpy((np.exp2(np.add(POWERS, shift))[None, :, None] * u * np.ones((n, 1, 1))).astype(np.float32)).to(torch.bfloat16).cuda()
     qs = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+
+    def attend(q, scale, out):
+        if call == "prompt":
+            bl.prefill_attention(q, kp, vp, table, lens, qs, scale, out, k_scale=one, v_scale=one)
+        else:                       # the same rows, a request each of its own length
+            ones = None if one is None else one.expand(n, 1).contiguous()
+            bl.decode_attention(q, kp, vp, table.expand(n, P).contiguous(), lens - torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda"),
+                                scale, out, k_scale=ones, v_scale=ones)
     out, neg = (torch.full((n, G, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
-    bl.prefill_attention(q, kp, vp, table, lens, qs, scale, out, k_scale=one, v_scale=one)
-    bl.prefill_attention(-q, kp, vp, table, lens, qs, -scale, neg, k_scale=one, v_scale=one)
+    attend(q, scale, out)
+    attend(-q, -scale, neg)
     assert bl.device_errors() == 0
 
     seen = np.arange(L)[None, :] <= (L - n + np.arange(n))[:, None]

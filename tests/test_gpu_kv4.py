@@ -990,3 +990,62 @@ def test_a_page_outside_the_pool_takes_nothing_from_the_first(D, scale_byte):
         ref, mag, dot = kv4.attention(qf[first:first + n], *c.pools, c.table[b:b + 1], np.array([n], dtype=np.int32), [n], 0.1)
         close(out[first:first + n], ref, mag, dot, PROMPT, f"request {b}")
     assert torch.isnan(out[16:64]).all() and torch.isnan(out[128:]).all()
+
+
+def test_one_call_step_captured_and_replayed():
+    """bellman_decode_step over 4-bit pools from a graph, a growing batch, with
+    eager calls on a second cache between the replays; a refused call leaves
+    pools and lengths alone."""
+    lens, H, G, D, steps = [30, 1, 500, 64, 0], 2, 4, 64, 4
+    a, b = (Cache(np.random.default_rng(3), lens, H, D, room=steps + 1).to_device() for _ in range(2))
+    rows = torch.randn((steps, 5, (G + 2) * H, D), device="cuda").to(torch.bfloat16)
+    cur, outs = rows[0].clone(), [torch.full((5, G * H, D), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def step(c, x, out):
+        bl.decode_step(x[:, G * H:-H], x[:, -H:], x[:, :G * H], c.k, c.v, c.bt, c.sl, 0.1, out)
+    before = a.bytes()
+    with pytest.raises(bl.BellmanError):
+        step(a, cur, torch.empty((5, G * H + 1, D), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(bl.BellmanError):
+        bl.decode_step(cur[:, G * H:-H], cur[:, -H - 1:], cur[:, :G * H], a.k, a.v, a.bt, a.sl, 0.1, outs[0])
+    torch.cuda.synchronize()
+    assert all(np.array_equal(x, y) for x, y in zip(before, a.bytes())) and a.sl.tolist() == lens
+    bl.decode_attention(cur[:, :G * H], a.k, a.v, a.bt, a.sl, 0.1, outs[0])          # the workspace grows
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(a, cur, outs[0])
+    for i in range(steps):
+        cur.copy_(rows[i])
+        g.replay()
+        step(b, rows[i], outs[1])
+        torch.cuda.synchronize()
+        assert torch.equal(*outs) and not torch.isnan(outs[0]).any()
+        assert all(np.array_equal(x, y) for x, y in zip(a.bytes(), b.bytes()))
+    assert torch.equal(a.sl, b.sl) and a.sl.tolist() == [n + steps for n in lens] and bl.device_errors() == 0
+
+
+@pytest.mark.parametrize("B", [64, 65, 200])      # planned in the waves, and by a launch
+def test_read_of_malformed_requests_among_many(B):
+    rng = np.random.default_rng(B)
+    lens = rng.integers(1, 40, B)
+    c = Cache(rng, lens, 1, 64)
+    n = np.minimum(lens, rng.integers(0, 40, B))
+    n[5] = lens[5] + 1                              # more rows than it has
+    c.lens[7] = 16 * c.table.shape[1] + 1           # past the table
+    c.lens[9] = -3
+    c.to_device()
+    at = np.concatenate([[0], np.cumsum(n)])
+    ko, vo = (torch.full((int(at[-1]) + 2, 1, 64), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    bl.kv_read(c.k, c.v, c.bt, c.sl, dev(at.astype(np.int32)), ko, vo)
+    assert bl.device_errors() == 2
+    for got, pool, kind in ((ko, c.pools[0], "k"), (vo, c.pools[1], "v")):
+        got = got.double().cpu().numpy()
+        for b in range(B):
+            rows = got[at[b]:at[b + 1]]
+            if b in (5, 7, 9):
+                assert (rows == 5).all()
+            else:
+                L = int(lens[b])
+                assert np.array_equal(rows, kv4.read_pages(pool, c.table[b, :(L + 15) // 16], kind)[L - n[b]:L])
+        assert (got[at[-1]:] == 5).all()
