@@ -228,7 +228,8 @@ typedef struct bellman_attn_opts {
                              untraced call.  Built for bf16 and fp8 pools of
                              head_dim 128 at the default steps (bf16:
                              pages_per_step 1 or 2 with pipeline_depth 0 or 2;
-                             fp8: 4 pages, depth 1); other shapes return BELLMAN_ERR_UNSUPPORTED.  NULL = none */
+                             fp8: 4 pages, depth 1); other shapes return
+                             BELLMAN_ERR_UNSUPPORTED.  NULL = none */
 } bellman_attn_opts_t;
 
 /* bellman_decode_attention with explicit tuning options (NULL = defaults).
@@ -419,8 +420,8 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * into the workspace as fp16, each 64-token step of a (request, KV head) at
  * the power of two 2^e that brings its largest magnitude M into
  * [2^14, 2^15): every value of at least M 2^-28 converts exactly, smaller ones
- * keep an absolute error below M 2^-40, none overflows; the output is kept at the finest step's scale, a coarser step's
- * weights are multiplied by the difference, and 2^-e is taken out at the end
+ * keep an absolute error below M 2^-40, none overflows; the output is kept at
+ * the finest step's scale, a coarser step's weights are multiplied by the difference, and 2^-e is taken out at the end
  * (values more than 2^63 below the largest of a key range lose bits).  Over fp8 pools the
  * codes are staged in LDS as bytes and widened exactly at the operand load
  * (K to bf16, V to fp16); the K scale folds into the softmax scale and the
