@@ -421,8 +421,9 @@ int bellman_qk_norm_rope(const bellman_tensor_t *q, const bellman_tensor_t *k,
  * the power of two 2^e that brings its largest magnitude M into
  * [2^14, 2^15): every value of at least M 2^-28 converts exactly, smaller ones
  * keep an absolute error below M 2^-40, none overflows; the output is kept at
- * the finest step's scale, a coarser step's weights are multiplied by the difference, and 2^-e is taken out at the end
- * (values more than 2^63 below the largest of a key range lose bits).  Over fp8 pools the
+ * the finest step's scale, a coarser step's weights are multiplied by the
+ * difference, and 2^-e is taken out at the end (values more than 2^63 below the
+ * largest of a key range lose bits).  Over fp8 pools the
  * codes are staged in LDS as bytes and widened exactly at the operand load
  * (K to bf16, V to fp16); the K scale folds into the softmax scale and the
  * V scale into the final normalisation.  Over 4-bit pools the keys enter the

@@ -1107,9 +1107,9 @@ constexpr int kValuPerMfma = 7;
 // scaled by a power of two a column and 32 dims (lane (h, c): k = 16 h + 0..15 and
 // 32 + 16 h + 0..15, and the scale of k = 32 h .. 32 h + 31), exact for bf16 within
 // 2^-14 of the block's largest: two products of 64 dims at twice bf16's rate.
-// Values come from the fp16 copy.  Widening the keys
-// to bf16 in LDS instead: eight chats' 16-256 new tokens after 2-8k 122 us, not
-// 112, four 2,048-token chunks after 4-10k 1049, not 996-1019 (whole calls).
+// Values come from the fp16 copy.  Widening the keys to bf16 in LDS instead: eight
+// chats' 16-256 new tokens after 2-8k 122 us, not 112, four 2,048-token chunks after
+// 4-10k 1049, not 996-1019 (whole calls).
 template <int D, int NH, bool FP8, bool FP4>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_attn_kernel(PrefillArgs a) {
